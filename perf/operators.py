@@ -142,7 +142,7 @@ def prepare(case, seed):
         state["out"] = torch.zeros((tokens, heads, dim), dtype=dtype, device=GPU)
     if own:
         import paper_2508_01989_amd as tc
-        pool = tc.make_kv8_pool(heads, kv_heads, dim, blocks, state["k"], state["v"], state["scales"],
+        pool = tc.make_kvq_pool(heads, kv_heads, dim, blocks, state["k"], state["v"], state["scales"],
                                 dtype=tc.TC_BF16 if case["dtype"] == "bf16" else tc.TC_FP16)
         state["pool"], state["plan"] = pool, tc.Plan(pool, q_start, ctx.astype(np.int32), table)
         state["workspace"] = torch.empty(max(16, state["plan"].workspace_bytes), dtype=torch.uint8, device=GPU)
@@ -257,13 +257,13 @@ def run(state):
         import paper_2508_01989_amd as tc
         plan, pool = state["plan"], state["pool"]
         if kind == "append":
-            tc.tc_kv8_append(plan, pool, state["k_new"], state["v_new"])
+            tc.tc_kvq_append(plan, pool, state["k_new"], state["v_new"])
         elif kind == "read":
-            tc.tc_kv8_read(plan, pool, -1, state["k_out"], state["v_out"])
+            tc.tc_kvq_read(plan, pool, -1, state["k_out"], state["v_out"])
         elif kind == "attention":
-            tc.tc_kv8_mixed_attention(plan, pool, state["q"], state["out"], state["scale"], state["workspace"])
+            tc.tc_kvq_mixed_attention(plan, pool, state["q"], state["out"], state["scale"], state["workspace"])
         else:
-            tc.tc_kv8_mixed_attention_append(plan, pool, state["q"], state["k_new"], state["v_new"], state["out"], state["scale"], state["workspace"])
+            tc.tc_kvq_mixed_attention_append(plan, pool, state["q"], state["k_new"], state["v_new"], state["out"], state["scale"], state["workspace"])
     else:
         _plain(state)
     if kind == "read":
