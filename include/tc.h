@@ -49,6 +49,7 @@ typedef enum {
 
 #define TC_BF16 1
 #define TC_FP16 2 /* IEEE half: the precision the paper's own experiments ran in (Sec. 4.1) */
+#define TC_KV_E4M3 16 /* or-ed to one of them: the pools hold E4M3 bytes (tc_kvq_pool below) */
 
 /* Shape of the paged KV pool and where it lives. */
 typedef struct {
@@ -56,7 +57,8 @@ typedef struct {
     int32_t num_kv_heads; /* Hkv */
     int32_t head_dim;     /* 64 or 128 */
     int32_t block_size;   /* 16 */
-    int32_t dtype;        /* TC_BF16 or TC_FP16: element type of q, k, v, out and the pools */
+    int32_t dtype;        /* TC_BF16 or TC_FP16: element type of q, k, v, out and the pools; with TC_KV_E4M3 or-ed to it */
+                          /* the pools are those of a tc_kvq_pool                                                       */
     int64_t num_blocks;   /* blocks in each pool, num_blocks * 16 < 2^31 */
     void *k_pool;         /* DEVICE [num_blocks][Hkv][D/8][16][8] bf16; may be NULL for tc_plan_create* */
     void *v_pool;         /* DEVICE [num_blocks][Hkv][D][16] bf16                                        */
@@ -228,6 +230,53 @@ tc_status tc_attention_partials(const tc_plan *plan, const tc_kv_pool *pool, con
                                 void *workspace, size_t workspace_bytes, void *stream);
 tc_status tc_split_merge(const tc_plan *plan, const tc_kv_pool *pool, void *out, void *workspace,
                          size_t workspace_bytes, void *stream);
+
+/*
+ * The KV cache in 8 bits: half of the memory, and of the bytes that decodes read, per token.  K and V are held as E4M3
+ * numbers (four exponent and three mantissa bits, no infinity, largest magnitude 448) with one scale for each block
+ * and KV head, for K and for V, which is a power of two: byte b of a block stands for E4M3(b) * 2^e.
+ *   base.k_pool   [num_blocks][Hkv][D/16][B][16]           element d = 16 i + l of token t at [i][t][l]
+ *   base.v_pool   [num_blocks][Hkv][2][B/4][16][D/32][4]   element d = 32 c + 16 h + j of token 4 g + t at [h][g][j][c][t]
+ *   scales        [num_blocks][Hkv][2]                     e + 127 of the K block and of the V block
+ * The exponents are limited so that what a byte stands for is exact and finite in the element type of q, k_new, v_new and
+ * out: -117 <= e <= 120 for TC_BF16, -15 <= e <= 8 for TC_FP16, and at the highest e magnitudes end at 240.
+ *
+ * A plan for such pools is made from `base`, whose dtype has TC_KV_E4M3 or-ed to the element type; it serves the tc_kvq_
+ * calls, and the calls for pools in 16 bits reject it (and theirs these) with TC_ERR_SHAPE.  Work lists, workspace and rules
+ * of use are as described for tc_plan_create and tc_mixed_attention; arguments and errors are those of the calls without the 8, and:
+ * k_pool, v_pool, q, k_new, v_new, out and the outputs of tc_kvq_read are 16-byte aligned and scales 2-byte aligned
+ * (TC_ERR_ARG), and the current device is the plan's (TC_ERR_DEVICE).
+ */
+typedef struct {
+    tc_kv_pool base; /* k_pool, v_pool: DEVICE, one byte an element */
+    void *scales;    /* DEVICE [num_blocks][Hkv][2] uint8           */
+} tc_kvq_pool;
+
+/* Append to a cache in 8 bits: the new rows are quantised as they are written.  For each block that gets rows and each KV head,
+ * K and V apart, e becomes the smallest exponent (within the limits above) for which no finite new element of the block is beyond
+ * 448 * 2^e in magnitude, or the exponent the block had if that is larger and the sequence has earlier rows in the block.  A new
+ * element x becomes the E4M3 number nearest to x * 2^-e (ties to even; where limited, the largest); infinities and NaN become
+ * NaN.  Where e grows, the block's earlier rows are brought to it the same way, which changes only numbers below 2^-6 of the
+ * new scale.  What a block holds beyond the sequence's last token is left as it was.  A block that gets rows must belong
+ * to one sequence of the batch only; what the call leaves depends on the rows and the cache alone, and making it again changes
+ * nothing. */
+tc_status tc_kvq_append(const tc_plan *plan, const tc_kvq_pool *pool, const void *k_new, const void *v_new, void *stream);
+
+/* Read a cache in 8 bits back: k_out, v_out DEVICE [n][Hkv][D] get what tokens 0..ctx+q_len-1 of sequence `seq`, or of all
+ * sequences one after the other with seq = -1 (fewer than 2^31 tokens then), stand for.  Nothing is rounded.  Appending what was
+ * read to an empty block gives bytes that stand for the same numbers, and tc_kv_append of it a cache in 16 bits: this is how a
+ * request moves between instances whose caches differ. */
+tc_status tc_kvq_read(const tc_plan *plan, const tc_kvq_pool *pool, int32_t seq, void *k_out, void *v_out, void *stream);
+
+/* tc_mixed_attention over a cache in 8 bits: the same softmax over the numbers that the cache stands for, with the
+ * same accumulation and roundings. */
+tc_status tc_kvq_mixed_attention(const tc_plan *plan, const tc_kvq_pool *pool, const void *q, void *out, float scale,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/* tc_kvq_append and tc_kvq_mixed_attention of the same batch in one call; cache and outputs are bit for bit those of the two. */
+tc_status tc_kvq_mixed_attention_append(const tc_plan *plan, const tc_kvq_pool *pool, const void *q, const void *k_new,
+                                        const void *v_new, void *out, float scale, void *workspace, size_t workspace_bytes,
+                                        void *stream);
 
 /* Test hook: un-paged copy of tokens 0..ctx+q_len-1 of sequence `seq` out of the pool,
  * k_out / v_out DEVICE [kv_len][Hkv][D] bf16. */

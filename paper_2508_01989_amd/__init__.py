@@ -14,12 +14,13 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libtc_mi355x.so")
 
 TC_OK, TC_ERR_NULL, TC_ERR_SHAPE, TC_ERR_SPAN, TC_ERR_BLOCK, TC_ERR_WORKSPACE, TC_ERR_DEVICE, TC_ERR_ARG = range(8)
-TC_BF16, TC_FP16 = 1, 2
+TC_BF16, TC_FP16, TC_KV_E4M3 = 1, 2, 16
 
 EXPORTS = ["tc_plan_create", "tc_plan_create_host", "tc_plan_update", "tc_plan_get_info", "tc_plan_copy_items",
            "tc_plan_workspace_bytes", "tc_plan_destroy", "tc_kv_append", "tc_mixed_attention", "tc_mixed_attention_append",
            "tc_mixed_attention_static", "tc_attention_partials", "tc_split_merge",
            "tc_kv_gather", "tc_probe_mfma_loop", "tc_probe_stream_read", "tc_probe_stream_copy",
+           "tc_kvq_append", "tc_kvq_read", "tc_kvq_mixed_attention", "tc_kvq_mixed_attention_append",
            "tc_kv_transfer_bytes", "tc_kv_export", "tc_kv_import", "tc_status_str", "tc_last_error", "tc_version"]
 
 
@@ -27,6 +28,10 @@ class tc_kv_pool(C.Structure):
     _fields_ = [("num_q_heads", C.c_int32), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("block_size", C.c_int32), ("dtype", C.c_int32), ("num_blocks", C.c_int64),
                 ("k_pool", C.c_void_p), ("v_pool", C.c_void_p)]
+
+
+class tc_kvq_pool(C.Structure):
+    _fields_ = [("base", tc_kv_pool), ("scales", C.c_void_p)]
 
 
 class tc_batch(C.Structure):
@@ -80,6 +85,10 @@ def lib():
         L.tc_probe_stream_copy.argtypes = [vp, vp, C.c_size_t, vp]
         L.tc_split_merge.argtypes = [vp, C.POINTER(tc_kv_pool), vp, vp, C.c_size_t, vp]
         L.tc_kv_gather.argtypes = [vp, C.POINTER(tc_kv_pool), C.c_int32, vp, vp, vp]
+        L.tc_kvq_append.argtypes = [vp, C.POINTER(tc_kvq_pool), vp, vp, vp]
+        L.tc_kvq_read.argtypes = [vp, C.POINTER(tc_kvq_pool), C.c_int32, vp, vp, vp]
+        L.tc_kvq_mixed_attention.argtypes = [vp, C.POINTER(tc_kvq_pool), vp, vp, C.c_float, vp, C.c_size_t, vp]
+        L.tc_kvq_mixed_attention_append.argtypes = [vp, C.POINTER(tc_kvq_pool), vp, vp, vp, vp, C.c_float, vp, C.c_size_t, vp]
         L.tc_kv_transfer_bytes.argtypes = [vp, C.c_int32, C.c_int32]
         L.tc_kv_transfer_bytes.restype = C.c_size_t
         L.tc_kv_export.argtypes = [vp, C.POINTER(tc_kv_pool), C.c_int32, C.c_int32, C.POINTER(vp), C.POINTER(vp), vp, vp]
@@ -127,6 +136,18 @@ def make_pool(num_q_heads, num_kv_heads, head_dim, num_blocks, k_pool=None, v_po
     return tc_kv_pool(num_q_heads, num_kv_heads, head_dim, block_size, dtype, int(num_blocks), _ptr(k_pool), _ptr(v_pool))
 
 
+def make_kvq_pool(num_q_heads, num_kv_heads, head_dim, num_blocks, k_pool=None, v_pool=None, scales=None, block_size=16,
+                  dtype=TC_BF16) -> tc_kvq_pool:
+    """A cache in 8 bits; `dtype` is the element type of q, k_new, v_new and out.  Plan takes it as it takes a tc_kv_pool."""
+    return tc_kvq_pool(make_pool(num_q_heads, num_kv_heads, head_dim, num_blocks, k_pool, v_pool, block_size, dtype | TC_KV_E4M3),
+                       _ptr(scales))
+
+
+def _shape(pool):
+    """The tc_kv_pool that says the shape of either kind of pool."""
+    return pool.base if isinstance(pool, tc_kvq_pool) else pool
+
+
 def _batch(q_start, ctx_len, block_table):
     """tc_batch over contiguous int32 copies of the arrays (returned too: they must outlive the call)."""
     q_start = np.ascontiguousarray(q_start, np.int32)
@@ -139,11 +160,12 @@ def _batch(q_start, ctx_len, block_table):
 
 
 class Plan:
-    """Owner of a tc_plan handle.  Keeps nothing but the handle and its info."""
+    """Owner of a tc_plan handle.  Keeps nothing but the handle and its info.  pool: a tc_kv_pool or a tc_kvq_pool."""
 
-    def __init__(self, pool: tc_kv_pool, q_start, ctx_len, block_table, stream=None, host_only=False):
+    def __init__(self, pool, q_start, ctx_len, block_table, stream=None, host_only=False):
         batch, keep = _batch(q_start, ctx_len, block_table)
         h = C.c_void_p()
+        pool = _shape(pool)
         if host_only:
             _check(lib().tc_plan_create_host(C.byref(pool), C.byref(batch), C.byref(h)))
         else:
@@ -156,9 +178,10 @@ class Plan:
         _check(lib().tc_plan_get_info(self.handle, C.byref(info)))
         self.info = info
 
-    def update(self, pool: tc_kv_pool, q_start, ctx_len, block_table, stream=None):
+    def update(self, pool, q_start, ctx_len, block_table, stream=None):
         """tc_plan_update: re-plan this object for another batch, reusing its buffers."""
         batch, keep = _batch(q_start, ctx_len, block_table)
+        pool = _shape(pool)
         try:
             _check(lib().tc_plan_update(self.handle, C.byref(pool), C.byref(batch), _stream(stream)))
         finally:
@@ -237,6 +260,29 @@ def tc_split_merge(plan: Plan, pool: tc_kv_pool, out, workspace=None, workspace_
 
 def tc_kv_gather(plan: Plan, pool: tc_kv_pool, seq, k_out, v_out, stream=None):
     _check(lib().tc_kv_gather(plan.handle, C.byref(pool), int(seq), _ptr(k_out), _ptr(v_out), _stream(stream)))
+
+
+def tc_kvq_append(plan: Plan, pool: tc_kvq_pool, k_new, v_new, stream=None):
+    _check(lib().tc_kvq_append(plan.handle, C.byref(pool), _ptr(k_new), _ptr(v_new), _stream(stream)))
+
+
+def tc_kvq_read(plan: Plan, pool: tc_kvq_pool, seq, k_out, v_out, stream=None):
+    _check(lib().tc_kvq_read(plan.handle, C.byref(pool), int(seq), _ptr(k_out), _ptr(v_out), _stream(stream)))
+
+
+def tc_kvq_mixed_attention(plan: Plan, pool: tc_kvq_pool, q, out, scale, workspace=None, workspace_bytes=None, stream=None):
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().tc_kvq_mixed_attention(plan.handle, C.byref(pool), _ptr(q), _ptr(out), C.c_float(scale), _ptr(workspace),
+                                        workspace_bytes, _stream(stream)))
+
+
+def tc_kvq_mixed_attention_append(plan: Plan, pool: tc_kvq_pool, q, k_new, v_new, out, scale, workspace=None,
+                                  workspace_bytes=None, stream=None):
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().tc_kvq_mixed_attention_append(plan.handle, C.byref(pool), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out),
+                                               C.c_float(scale), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def _ptr_array(pools):

@@ -160,7 +160,7 @@ extern "C" {
 
 size_t tc_kv_transfer_bytes(const tc_plan *plan, int32_t seq, int32_t num_layers) {
     int page0 = 0, n = 0;
-    if (!plan || num_layers < 1 || num_layers > tc::kMaxLayers || !selection(plan, seq, &page0, &n)) return 0;
+    if (!plan || plan->kvq || num_layers < 1 || num_layers > tc::kMaxLayers || !selection(plan, seq, &page0, &n)) return 0;
     return (size_t)num_layers * (size_t)n * 2 * (size_t)plan->Hkv * tc::kBlock * (size_t)plan->D * sizeof(uint16_t);
 }
 
@@ -172,6 +172,95 @@ tc_status tc_kv_export(const tc_plan *plan, const tc_kv_pool *pool, int32_t seq,
 tc_status tc_kv_import(const tc_plan *plan, const tc_kv_pool *pool, int32_t seq, int32_t num_layers,
                        void *const *k_pools, void *const *v_pools, const void *buffer, void *stream) {
     return migrate(plan, pool, seq, num_layers, k_pools, v_pools, (void *)buffer, stream, true);
+}
+
+}  // extern "C"
+
+// ---- the KV cache in 8 bits
+
+namespace {
+
+bool misaligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
+tc_status check_kvq(const tc_plan *plan, const tc_kvq_pool *pool) {
+    if (!plan || !pool) return fail(TC_ERR_NULL, "plan or pool is NULL");
+    tc_status st = tc::check_pool_matches(plan, &pool->base, true, true);
+    if (st != TC_OK) return st;
+    if (!pool->scales) return fail(TC_ERR_NULL, "scales is NULL");
+    if (misaligned(pool->base.k_pool, 16) || misaligned(pool->base.v_pool, 16) || misaligned(pool->scales, 2))
+        return fail(TC_ERR_ARG, "k_pool and v_pool must be 16-byte aligned, scales 2-byte");
+    return TC_OK;
+}
+
+tc_status check_kvq_device(const tc_plan *plan) {  // last, so that a plan without a device copy shows every other mistake
+    if (!plan->dev) return fail(TC_ERR_ARG, "plan was built host-only (tc_plan_create_host) and cannot be launched");
+    int device = -1;
+    if (int err = tc::current_device(&device)) return device_result(err, "current device");
+    if (device != plan->device) return fail(TC_ERR_DEVICE, "the current device is not the one the plan was made on");
+    return TC_OK;
+}
+
+tc_status check_kvq_rows(const void *k_new, const void *v_new) {
+    if (!k_new || !v_new) return fail(TC_ERR_NULL, "k_new or v_new is NULL");
+    if (misaligned(k_new, 16) || misaligned(v_new, 16)) return fail(TC_ERR_ARG, "k_new and v_new must be 16-byte aligned");
+    return TC_OK;
+}
+
+tc_status check_kvq_attention(const tc_plan *plan, const void *q, const void *out, float scale, const void *workspace, size_t workspace_bytes) {
+    if (!q || !out) return fail(TC_ERR_NULL, "q or out is NULL");
+    if (misaligned(q, 16) || misaligned(out, 16)) return fail(TC_ERR_ARG, "q and out must be 16-byte aligned");
+    const size_t need = plan->workspace_bytes();
+    if (need > 0 && (!workspace || workspace_bytes < need)) return fail(TC_ERR_WORKSPACE, "workspace missing or too small");
+    if (need > 0 && misaligned(workspace, 16)) return fail(TC_ERR_ARG, "workspace must be 16-byte aligned");
+    if (!(scale > 0.f) || scale > 3.0e38f) return fail(TC_ERR_ARG, "scale must be positive and finite");
+    return TC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+tc_status tc_kvq_append(const tc_plan *plan, const tc_kvq_pool *pool, const void *k_new, const void *v_new, void *stream) {
+    tc_status st = check_kvq(plan, pool);
+    if (st != TC_OK || plan->T == 0) return st;
+    if ((st = check_kvq_rows(k_new, v_new)) != TC_OK || (st = check_kvq_device(plan)) != TC_OK) return st;
+    return device_result(tc::launch_kvq_append(plan, pool, k_new, v_new, stream), "tc_kvq_append launch");
+}
+
+tc_status tc_kvq_read(const tc_plan *plan, const tc_kvq_pool *pool, int32_t seq, void *k_out, void *v_out, void *stream) {
+    tc_status st = check_kvq(plan, pool);
+    if (st != TC_OK) return st;
+    int page0 = 0, n = 0;
+    if (!selection(plan, seq, &page0, &n)) return fail(TC_ERR_ARG, "sequence index out of range");
+    if (n == 0) return TC_OK;
+    if (!k_out || !v_out) return fail(TC_ERR_NULL, "k_out or v_out is NULL");
+    if (misaligned(k_out, 16) || misaligned(v_out, 16)) return fail(TC_ERR_ARG, "k_out and v_out must be 16-byte aligned");
+    if (seq == -1) {
+        int64_t tokens = plan->T;
+        for (int s = 0; s < plan->S; s++) tokens += plan->ctx_len[s];
+        if (tokens >= (int64_t)1 << 31) return fail(TC_ERR_ARG, "2^31 tokens or more: read the sequences one by one");
+    }
+    if ((st = check_kvq_device(plan)) != TC_OK) return st;
+    return device_result(tc::launch_kvq_read(plan, pool, page0, n, k_out, v_out, stream), "tc_kvq_read launch");
+}
+
+tc_status tc_kvq_mixed_attention(const tc_plan *plan, const tc_kvq_pool *pool, const void *q, void *out, float scale, void *workspace,
+                                 size_t workspace_bytes, void *stream) {
+    tc_status st = check_kvq(plan, pool);
+    if (st != TC_OK || plan->T == 0) return st;
+    if ((st = check_kvq_attention(plan, q, out, scale, workspace, workspace_bytes)) != TC_OK || (st = check_kvq_device(plan)) != TC_OK) return st;
+    return device_result(tc::launch_kvq_attention(plan, pool, q, out, scale, workspace, stream), "tc_kvq_mixed_attention launch");
+}
+
+tc_status tc_kvq_mixed_attention_append(const tc_plan *plan, const tc_kvq_pool *pool, const void *q, const void *k_new, const void *v_new,
+                                        void *out, float scale, void *workspace, size_t workspace_bytes, void *stream) {
+    tc_status st = check_kvq(plan, pool);
+    if (st != TC_OK || plan->T == 0) return st;
+    if ((st = check_kvq_rows(k_new, v_new)) != TC_OK) return st;
+    if ((st = check_kvq_attention(plan, q, out, scale, workspace, workspace_bytes)) != TC_OK || (st = check_kvq_device(plan)) != TC_OK) return st;
+    st = device_result(tc::launch_kvq_append(plan, pool, k_new, v_new, stream), "tc_kvq_mixed_attention_append launch");
+    if (st != TC_OK) return st;
+    return device_result(tc::launch_kvq_attention(plan, pool, q, out, scale, workspace, stream), "tc_kvq_mixed_attention_append launch");
 }
 
 }  // extern "C"

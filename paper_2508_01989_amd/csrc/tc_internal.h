@@ -86,6 +86,7 @@ struct PlanScratch {
 struct tc_plan {
     int Hq = 0, Hkv = 0, D = 0, G = 0;
     int dtype = TC_BF16;  // element type of q / k / v / out: selects the MFMA instantiation
+    bool kvq = false;     // the pools hold 8 bits an element (TC_KV_E4M3): a plan is for one kind of pools
     int64_t num_blocks = 0;
     int S = 0, T = 0;
     int n_prefill_seqs = 0, n_decode_seqs = 0;
@@ -109,8 +110,8 @@ struct tc_plan {
     int32_t *host = nullptr;
     size_t host_n = 0, host_cap = 0;
     bool host_pinned = false;
-    size_t off_records = 0, off_append = 0, off_pages = 0, off_valid = 0, off_prefill = 0, off_decode = 0, off_merge = 0,
-           off_counters = 0;  // off_valid: tokens (1..16) each page holds
+    size_t off_records = 0, off_append = 0, off_pages = 0, off_valid = 0, off_rows = 0, off_prefill = 0, off_decode = 0, off_merge = 0,
+           off_counters = 0;  // off_valid: tokens (1..16) each page holds; off_rows (pools of 8 bits): tokens before it, of all sequences
     int n_append = 0;  // (sequence, page) segments written by the append
     int n_append_prefill = 0;  // the first of them are those of the prefill chunks
     bool on_device = false;  // the plan keeps a device copy (tc_plan_create); false for tc_plan_create_host
@@ -138,7 +139,7 @@ namespace tc {
 // Validate the batch and rebuild the host side of `plan` for it.  Returns TC_OK or an error (text via
 // set_error); after an error the plan describes an empty batch.
 tc_status build_plan(tc_plan *plan, const tc_kv_pool *pool, const tc_batch *batch);
-tc_status check_pool_matches(const tc_plan *plan, const tc_kv_pool *pool, bool need_ptrs);
+tc_status check_pool_matches(const tc_plan *plan, const tc_kv_pool *pool, bool need_ptrs, bool kvq = false);
 
 // Kernel launchers (tc_kernels.hip).  All return hipError_t as int (0 = success).
 // only_prefill: store the rows of the prefill chunks only (the decode rows are stored by the attention kernel).
@@ -156,6 +157,11 @@ int static_scratch(int device, void **ptr, size_t *bytes);
 // Pool <-> transfer buffer copy of the pages [page0, page0 + n_pages) of the plan, all layers.
 int launch_kv_migrate(const tc_plan *p, bool import, int page0, int n_pages, int num_layers, void *const *k_pools,
                       void *const *v_pools, void *buffer, void *stream);
+// A cache in 8 bits (tc_kvq.hip).
+int launch_kvq_append(const tc_plan *p, const tc_kvq_pool *pool, const void *k_new, const void *v_new, void *stream);
+int launch_kvq_read(const tc_plan *p, const tc_kvq_pool *pool, int page0, int n_pages, void *k_out, void *v_out, void *stream);
+int launch_kvq_attention(const tc_plan *p, const tc_kvq_pool *pool, const void *q, void *out, float scale, void *workspace, void *stream);
+int current_device(int *device);
 // Host image of a plan: wait until the latest upload has read it, then make room for n int32 (pinned
 // memory when the plan has a device copy).
 int begin_plan_host(tc_plan *p, size_t n);

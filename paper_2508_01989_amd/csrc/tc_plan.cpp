@@ -20,10 +20,12 @@ static tc_status fail(tc_status s, const std::string &msg) {
     return s;
 }
 
-tc_status check_pool_matches(const tc_plan *plan, const tc_kv_pool *pool, bool need_ptrs) {
+tc_status check_pool_matches(const tc_plan *plan, const tc_kv_pool *pool, bool need_ptrs, bool kvq) {
     if (!plan || !pool) return fail(TC_ERR_NULL, "plan or pool is NULL");
+    if (plan->kvq != kvq)
+        return fail(TC_ERR_SHAPE, kvq ? "this call needs a plan for pools of 8 bits (TC_KV_E4M3)" : "the plan is for pools of 8 bits: use the tc_kvq_ calls");
     if (pool->num_q_heads != plan->Hq || pool->num_kv_heads != plan->Hkv || pool->head_dim != plan->D ||
-        pool->block_size != kBlock || pool->num_blocks != plan->num_blocks || pool->dtype != plan->dtype)
+        pool->block_size != kBlock || pool->num_blocks != plan->num_blocks || pool->dtype != (plan->dtype | (kvq ? TC_KV_E4M3 : 0)))
         return fail(TC_ERR_SHAPE, "pool shape differs from the shape the plan was built for");
     if (need_ptrs && (!pool->k_pool || !pool->v_pool)) return fail(TC_ERR_NULL, "k_pool or v_pool is NULL");
     return TC_OK;
@@ -529,7 +531,9 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     p->total_pages = 0;
     p->host_n = 0;
     const int Hq = pool->num_q_heads, Hkv = pool->num_kv_heads, D = pool->head_dim;
-    if (pool->dtype != TC_BF16 && pool->dtype != TC_FP16) return fail(TC_ERR_SHAPE, "dtype must be TC_BF16 or TC_FP16");
+    const bool kvq = pool->dtype >= 0 && (pool->dtype & TC_KV_E4M3);
+    const int dtype = kvq ? pool->dtype & ~TC_KV_E4M3 : pool->dtype;
+    if (dtype != TC_BF16 && dtype != TC_FP16) return fail(TC_ERR_SHAPE, "dtype must be TC_BF16 or TC_FP16, and TC_KV_E4M3 or-ed to it for pools of 8 bits");
     if (pool->block_size != kBlock) return fail(TC_ERR_SHAPE, "block_size must be 16");
     if (D != 64 && D != 128) return fail(TC_ERR_SHAPE, "head_dim must be 64 or 128");
     if (Hkv <= 0 || Hq <= 0 || Hq % Hkv) return fail(TC_ERR_SHAPE, "num_q_heads must be a positive multiple of num_kv_heads");
@@ -538,7 +542,7 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     if (G > 16) return fail(TC_ERR_SHAPE, "more than 16 query heads per KV head is not supported");
     if (pool->num_blocks <= 0 || pool->num_blocks * kBlock >= (int64_t)1 << 31)
         return fail(TC_ERR_SHAPE, "num_blocks must be in [1, 2^27)");
-    p->Hq = Hq; p->Hkv = Hkv; p->D = D; p->G = G; p->dtype = pool->dtype; p->num_blocks = pool->num_blocks;
+    p->Hq = Hq; p->Hkv = Hkv; p->D = D; p->G = G; p->dtype = dtype; p->kvq = kvq; p->num_blocks = pool->num_blocks;
     if (b->num_seqs < 0) return fail(TC_ERR_SPAN, "negative num_seqs");
     const int S = b->num_seqs;
     if (S > 0 && (!b->q_start || !b->ctx_len || !b->block_table)) return fail(TC_ERR_NULL, "a batch array is NULL");
@@ -577,7 +581,7 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     PlanScratch &w = p->work;
 
     // ---- prefill row blocks, heaviest (latest positions, longest KV range) first, and their pieces
-    const int64_t decode_bytes = decode_tokens * Hkv * D * 4;
+    const int64_t decode_bytes = decode_tokens * Hkv * D * (kvq ? 2 : 4);
     p->rows_per_item = choose_rows_per_item(p, S, decode_bytes);
     make_row_blocks(p, S, p->rows_per_item, w.blocks);
     // The sweeps in runs, at most `bins` per KV head: the number made, or 0 (the blocks as they were) where runs whose regions
@@ -614,7 +618,7 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
             // sixteen of 51 (384) 15.2 / 12.8; head_dim 64, 32/8 heads, 1000 at 0 (256) 18.0 / 17.1, 816 (208) 15.3 / 15.1.  Not where every item has a
             // unit to itself at head_dim 128 (32/8 heads, 1000 at 0 24.3 / 25.0, 816 21.4 / 22.0), nor beside decodes, of which eight
             // waves carry more at a time (972 at 0 with 2 25.2 / 26.4; 19 at 737 with 15 17.9 / 18.6).
-            if (decode_tokens == 0 && items > (D == 64 ? kNumCu / 2 : kNumCu)) p->prefill_waves = kSmallWaves;
+            if (!kvq && decode_tokens == 0 && items > (D == 64 ? kNumCu / 2 : kNumCu)) p->prefill_waves = kSmallWaves;
             // (Items of 128 rows take their unit for half as long: they have a queue from half of the units on.  On fewer units drawing
             // from it costs more than it levels: 270 first tokens with 3 decodes of 100-300, 32/8 heads, in 72 items, without it /
             // with it 15.3 / 16.8 us; at head_dim 64 with 46 of 30-300 12.0 / 13.7; 500 tokens, 128 items, with 16 of 100-900 19.0 / 20.8.)
@@ -634,6 +638,7 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
             // Small workgroups: beside more decodes the queue fills the units whose sweeps end early; long sweeps run at a lower clock in either
             // form than the estimates say (6562 at 16848, 8/8 heads, 526 / 543).
             const double small_below = (w.blocks[0].n_tiles <= 64 ? 0.97 : 0.9) * t_whole;
+            if (kvq) t.small = 1e30;  // (the tiles of small workgroups in 16 bits and the pages in 8 do not fit the LDS of a unit)
             bool small = t.small < small_below && t_decode < 0.05 * t.small;
             // That is by a unit's share of all sweeps.  Where some units have two long ones it is theirs that count, a tile of the fullest unit 0.9 us, 0.5 at
             // head_dim 64; for sweeps of up to 24 tiles it makes no difference.  (whole / small:) 16/2 heads, 2652 at 11274 and 2355 at 0 with 5
@@ -748,7 +753,7 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
         for (int s = 0; s < S; s++)
             if (p->q_start[s + 1] - p->q_start[s] == 1) longest = std::max(longest, (int64_t)p->ctx_len[s] + 1);
         for (const PlanRowBlock &x : w.blocks) cut |= x.k > 1;
-        if (p->waves_per_item == 1 && p->prefill_waves == kMixedWaves && !queue && !cut && longest <= 768 && (int64_t)n_decode_seqs * Hkv * 2 >= kNumCu && decode_bytes < (int64_t)600000000 &&
+        if (!kvq && p->waves_per_item == 1 && p->prefill_waves == kMixedWaves && !queue && !cut && longest <= 768 && (int64_t)n_decode_seqs * Hkv * 2 >= kNumCu && decode_bytes < (int64_t)600000000 &&
             (int64_t)w.blocks.size() * Hkv * 4 <= kNumCu) {
             p->prefill_waves = p->items_per_wg = kSmallWaves;
             p->rows_per_item = kPrefillRows / 2;
@@ -864,7 +869,8 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     const size_t off_records = 0;  // first: a record is a 128-byte line
     const size_t off_append = w.pieces.size() * kRecordInts, off_pages = off_append + (size_t)n_append * kAppendInts;
     const size_t off_valid = off_pages + (size_t)pages;
-    const size_t off_prefill = off_valid + (size_t)pages;
+    const size_t off_rows = off_valid + (size_t)pages;
+    const size_t off_prefill = off_rows + (kvq ? (size_t)pages : 0);
     const size_t off_decode = off_prefill + (size_t)n_prefill * kItemInts;
     const size_t off_merge = off_decode + (size_t)n_decode * kItemInts;
     const size_t off_counters = (off_merge + (size_t)n_merge * kItemInts + kCounterLine - 1) / kCounterLine * kCounterLine;
@@ -885,6 +891,13 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
         int32_t *val = H + off_valid + p->page_off[s];
         for (int i = 0; i + 1 < np; i++) val[i] = kBlock;
         val[np - 1] = kv - (np - 1) * kBlock;
+    }
+    if (kvq) {  // (past 2^31 tokens the sum wraps: tc_kvq_read refuses all sequences at once then, and takes differences within one)
+        uint32_t before = 0;
+        for (int64_t i = 0; i < pages; i++) {
+            H[off_rows + i] = (int32_t)before;
+            before += (uint32_t)H[off_valid + i];
+        }
     }
     {   // append segments: those of the prefill chunks first (the call that fuses the append into the attention
         // kernel still stores the chunks' rows with the append kernel, and only those)
@@ -1019,7 +1032,7 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     p->n_merge = (int)n_merge; p->n_partials = (int)n_partials; p->n_counters = (int)n_counters; p->n_append = (int)n_append;
     p->n_piece_partials = (int)n_piece_partials; p->n_merge_prefill = (int)n_merge_prefill;
     p->n_decode_wg = (int)n_decode_wg; p->n_dealt = (int)n_dealt; p->n_drawers = (int)n_drawers; p->counter_stride = counter_stride; p->queue_counter = queue || late_queue ? (int)off_queue : -1;
-    p->off_records = off_records; p->off_append = off_append; p->off_pages = off_pages; p->off_valid = off_valid; p->off_prefill = off_prefill;
+    p->off_records = off_records; p->off_append = off_append; p->off_pages = off_pages; p->off_valid = off_valid; p->off_rows = off_rows; p->off_prefill = off_prefill;
     p->off_decode = off_decode; p->off_merge = off_merge; p->off_counters = off_counters;
     p->host_n = total;
     return TC_OK;

@@ -1,0 +1,222 @@
+"""The KV cache in 8 bits on the GPU, through the C ABI, against the plain form in 64 bits (oracle/kvq.py): bytes and exponents of the cache
+equal, what is read back equal, attention within a bound that counts its roundings.
+
+The bound: probabilities and outputs are rounded to nearest in the element type (half a step, h = eps / 2, relative), sums are
+held in 32 bits.  With a = sum_j p_j |v_j| / sum_j p_j the rounding of p moves an output by at most h a and its own rounding by at
+most h |out|.  A probability of IEEE half below 2^-14 of the reference is rounded in steps of 2^-24 instead, which adds at most 2^-25 |v|
+per key, and the probabilities' sum is at least about one.  32-bit arithmetic (score products, exponentials, sums) adds less than a fiftieth of h."""
+import zlib
+
+import numpy as np
+import pytest
+
+import oracle
+from oracle import kvq
+
+pytestmark = pytest.mark.gpu
+HALF_STEP = {"bf16": 2.0 ** -8, "fp16": 2.0 ** -11}
+
+
+@pytest.fixture(scope="module")
+def tc():
+    import torch
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    import paper_2508_01989_amd as m
+    return m
+
+
+def bits_of(x, dtype):
+    if dtype == "fp16":
+        return x.astype(np.float16).view(np.uint16)
+    u = np.ascontiguousarray(x, np.float32).view(np.uint32)
+    return ((u + 0x7FFF + ((u >> 16) & 1)) >> 16).astype(np.uint16)
+
+
+class Case:
+    """A batch with a history, its tensors (uint16 patterns) and block tables; rows of very different magnitudes, so that scales grow."""
+
+    def __init__(self, name, Hq, Hkv, D, q_len, ctx, dtype="bf16", spread=3, spare=3):
+        rng = np.random.default_rng(zlib.crc32(repr((name, dtype)).encode()))
+        self.name, self.Hq, self.Hkv, self.D, self.dtype = name, Hq, Hkv, D, dtype
+        self.q_len, self.ctx = np.array(q_len, np.int32), np.array(ctx, np.int32)
+        self.S, self.kv = len(q_len), self.q_len + self.ctx
+        self.q_start = np.concatenate([[0], np.cumsum(self.q_len)]).astype(np.int32)
+        self.h_start = np.concatenate([[0], np.cumsum(self.ctx)]).astype(np.int32)
+        pages = -(-self.kv // 16)
+        self.blocks = int(pages.sum()) + spare
+        ids = rng.permutation(self.blocks).astype(np.int32)
+        self.table = np.zeros((self.S, int(pages.max())), np.int32)
+        at = 0
+        for s, n in enumerate(pages):
+            self.table[s, :n] = ids[at:at + n]
+            at += n
+        T, P = int(self.q_start[-1]), int(self.h_start[-1])
+
+        def rows(n, heads):
+            x = rng.standard_normal((n, heads, D), np.float32) * np.exp2(rng.integers(-spread, 1, (n, heads, 1))).astype(np.float32)
+            return bits_of(x, dtype)
+
+        self.q = bits_of(rng.standard_normal((T, Hq, D), np.float32) * 1.5, dtype)
+        self.k_new, self.v_new, self.k_hist, self.v_hist = rows(T, Hkv), rows(T, Hkv), rows(P, Hkv), rows(P, Hkv)
+        self.scale = float(np.float32(1.0 / np.sqrt(D)))
+
+    def oracle_cache(self, new=True):
+        c = kvq.Cache(self.blocks, self.Hkv, self.D, self.dtype)
+        has = np.flatnonzero(self.ctx > 0)
+        for s in has:
+            a, b = self.h_start[s], self.h_start[s + 1]
+            c.append([0, b - a], [0], self.table[s:s + 1], self.k_hist[a:b], self.v_hist[a:b])
+        if new:
+            c.append(self.q_start, self.ctx, self.table, self.k_new, self.v_new)
+        return c
+
+    def attention(self, cache, rows=None):
+        """Outputs in 64 bits and the bound of this module's text."""
+        code = oracle.FP16 if self.dtype == "fp16" else oracle.BF16
+        kp, vp = cache.widened_pools(self.table, self.kv)
+        args = (self.Hq, self.Hkv, self.D, 16, self.q_start, self.ctx, self.table, self.q, self.scale, rows)
+        out = oracle.attention(kp, vp, *args, dtype=code)
+        a = oracle.attention(kp, vp & np.uint16(0x7FFF), *args, dtype=code)
+        bound = HALF_STEP[self.dtype] * 1.02 * (a + np.abs(out))
+        if self.dtype == "fp16":
+            v_max = max(float(np.abs(kvq.widen(x, "fp16")).max()) for x in (self.v_new, self.v_hist) if x.size)
+            bound += int(self.kv.max()) * 2.0 ** -25 * v_max
+        return out, bound + 1e-30
+
+
+class Device:
+    def __init__(self, tc, c, device="cuda:0", stream=None, poison=0x7F):
+        import torch
+        self.tc, self.c, self.torch = tc, c, torch
+        self.stream = stream
+        up = lambda a: torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).to(device)  # noqa: E731
+        n = c.blocks * c.Hkv * 16 * c.D
+        self.k, self.v = (torch.full((n,), poison, dtype=torch.uint8, device=device) for _ in range(2))
+        self.scales = torch.full((c.blocks * c.Hkv * 2,), 0xFF, dtype=torch.uint8, device=device)
+        self.pool = tc.make_kvq_pool(c.Hq, c.Hkv, c.D, c.blocks, self.k, self.v, self.scales, dtype=tc.TC_FP16 if c.dtype == "fp16" else tc.TC_BF16)
+        self.q, self.k_new, self.v_new, kh, vh = (up(x) for x in (c.q, c.k_new, c.v_new, c.k_hist, c.v_hist))
+        has = np.flatnonzero(c.ctx > 0)
+        if len(has):
+            start = np.concatenate([[0], np.cumsum(c.ctx[has])]).astype(np.int32)
+            plan = tc.Plan(self.pool, start, np.zeros(len(has), np.int32), c.table[has])
+            tc.tc_kvq_append(plan, self.pool, kh, vh)
+            torch.cuda.synchronize()
+            plan.destroy()
+        self.plan = tc.Plan(self.pool, c.q_start, c.ctx, c.table)
+        self.workspace = torch.full((max(16, self.plan.workspace_bytes),), 0xAB, dtype=torch.uint8, device=device)
+        self.out = torch.full((int(c.q_start[-1]) + 1, c.Hq, c.D), -1, dtype=torch.int16, device=device)  # a row more: nothing may write it
+        torch.cuda.synchronize()
+
+    def append(self):
+        self.tc.tc_kvq_append(self.plan, self.pool, self.k_new, self.v_new, stream=self.stream)
+
+    def attention(self):
+        self.tc.tc_kvq_mixed_attention(self.plan, self.pool, self.q, self.out, self.c.scale, self.workspace, stream=self.stream)
+
+    def step(self):
+        self.tc.tc_kvq_mixed_attention_append(self.plan, self.pool, self.q, self.k_new, self.v_new, self.out, self.c.scale, self.workspace,
+                                              stream=self.stream)
+
+    def cache(self):
+        self.torch.cuda.synchronize()
+        c = self.c
+        return tuple(x.cpu().numpy().reshape(c.blocks, c.Hkv, -1) for x in (self.k, self.v, self.scales))
+
+    def outputs(self):
+        self.torch.cuda.synchronize()
+        o = self.out.cpu().numpy().view(np.uint16)
+        assert (o[-1] == 0xFFFF).all(), "wrote behind the last row"
+        return kvq.widen(o[:-1], self.c.dtype)
+
+    def read(self, seq):
+        c, torch = self.c, self.torch
+        n = int(c.kv.sum() if seq < 0 else c.kv[seq])
+        k = torch.full((n + 1, c.Hkv, c.D), -1, dtype=torch.int16, device=self.k.device)
+        v = torch.full_like(k, -1)
+        self.tc.tc_kvq_read(self.plan, self.pool, seq, k, v, stream=self.stream)
+        torch.cuda.synchronize()
+        k, v = (x.cpu().numpy().view(np.uint16) for x in (k, v))
+        assert (k[-1] == 0xFFFF).all() and (v[-1] == 0xFFFF).all(), "wrote behind the last token"
+        return kvq.widen(k[:-1], c.dtype), kvq.widen(v[:-1], c.dtype)
+
+
+def check_cache(dev, cache, tag):
+    k, v, s = dev.cache()
+    assert np.array_equal(s, cache.scales), f"{tag}: exponents differ at {np.argwhere(s != cache.scales)[:4].tolist()}"
+    for name, got, want in (("K", k, cache.k), ("V", v, cache.v)):
+        bad = np.argwhere(got != want)
+        # the sign of a NaN is not defined
+        bad = [b for b in bad.tolist() if not (got[tuple(b)] & 0x7F == 0x7F and want[tuple(b)] & 0x7F == 0x7F)]
+        assert not bad, f"{tag}: {len(bad)} bytes of {name} differ, first {bad[:4]}"
+
+
+def check_attention(got, want, bound, tag):
+    assert np.array_equal(np.isnan(got), np.isnan(want)), f"{tag}: NaN in other places"
+    over = np.nan_to_num(np.abs(got - want) / bound)
+    assert over.max() <= 1.0, f"{tag}: {over.max():.3f} of the bound at {np.unravel_index(over.argmax(), over.shape)}"
+    return over.max()
+
+
+SHAPES = {
+    "one_token": (4, 1, 128, [1], [0]),
+    "page_boundaries": (8, 2, 128, [1, 1, 1, 1, 1], [14, 15, 16, 31, 32]),
+    "split_boundaries": (8, 2, 128, [1, 1, 1, 1], [126, 127, 128, 255]),
+    "decodes_ragged": (32, 8, 128, [1, 1, 1], [3000, 1025, 777]),
+    "decodes_of_every_length": (8, 2, 128, [1] * 70, list(range(70))),
+    "many_short_decodes": (8, 2, 64, [1] * 600, [(7 * i) % 41 for i in range(600)]),
+    "long_decode_many_partials": (8, 2, 128, [1, 1], [20000, 8191]),
+    "teams_g16": (16, 1, 128, [1, 1, 1], [5000, 3000, 700]),
+    "decodes_d64": (8, 2, 64, [1, 1, 1, 1, 1, 1], [100, 129, 600, 1500, 2047, 4100]),
+    "g16_d64": (16, 1, 64, [70, 1, 1], [40, 900, 17]),
+    "many_decodes_by_single_waves": (16, 8, 128, [1] * 96, [300 + 37 * i % 1100 for i in range(96)]),
+    "two_rows": (4, 1, 128, [2], [0]),
+    "ragged_chunk": (8, 2, 128, [77], [0]),
+    "chunk_inside_a_page": (8, 2, 128, [5, 3], [3, 20]),
+    "chunk_offset_unaligned": (8, 2, 128, [130], [37]),
+    "chunk_and_decodes": (8, 2, 128, [40, 1, 70, 1], [5, 99, 300, 0]),
+    "mha": (4, 4, 128, [300, 1], [20, 200]),
+    "g3": (6, 2, 128, [100, 1], [28, 75]),
+    "g5": (10, 2, 128, [120, 1], [0, 260]),
+    "three_kv_heads": (12, 3, 128, [50, 1, 1], [100, 300, 15]),
+    "five_kv_heads_d64": (5, 5, 64, [90, 1], [1200, 64]),
+    "d64_chunk": (8, 2, 64, [200, 1, 1], [45, 1000, 17]),
+    "sweeps_of_one_to_four_tiles": (8, 2, 128, [64, 65, 2, 30, 129, 1], [0, 0, 126, 99, 127, 5]),
+    "cut_chunk": (32, 8, 128, [64, 1], [5000, 50]),
+    "cut_d64": (4, 4, 64, [100, 1], [900, 30]),
+    "levelled_chunk": (32, 8, 128, [700], [900]),
+    "queue": (32, 8, 128, [520] + [1] * 24, [200] + [1500, 40, 2100, 900, 3300, 64] * 4),
+    "chunk_beside_long_decodes": (8, 2, 128, [33] + [1] * 4, [5] + [1023, 1024, 8191, 8192]),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("name", SHAPES)
+def test_step_against_the_plain_form(tc, name, dtype):
+    c = Case(name, *SHAPES[name], dtype=dtype)
+    print(f"[case] {name} {dtype}: S={c.S} T={int(c.q_start[-1])}", flush=True)
+    before, after = c.oracle_cache(new=False), c.oracle_cache()
+    dev = Device(tc, c)
+    check_cache(dev, before, "history")
+    dev.append()
+    check_cache(dev, after, "append")
+    dev.append()
+    check_cache(dev, after, "append again")
+    dev.attention()
+    want, bound = c.attention(after)
+    got = dev.outputs()
+    worst = check_attention(got, want, bound, name)
+    print(f"  worst {worst:.2f} of the bound", flush=True)
+    for s in sorted({0, c.S // 2, c.S - 1}):
+        for x, y in zip(dev.read(s), after.read(c.table[s], int(c.kv[s]))):
+            assert np.array_equal(x, y), f"sequence {s} read back"
+    for i, x in enumerate(dev.read(-1)):
+        y = np.concatenate([after.read(c.table[s], int(c.kv[s]))[i] for s in range(c.S)])
+        assert np.array_equal(x, y), "all sequences read back"
+    # both in one call, on a cache of its own: the same bits
+    one = Device(tc, c)
+    one.step()
+    check_cache(one, after, "step")
+    assert np.array_equal(one.outputs(), got)
+    one.step()
+    check_cache(one, after, "step again")
+    assert np.array_equal(one.outputs(), got)
