@@ -269,7 +269,7 @@ tc_status tc_kvq_append(const tc_plan *plan, const tc_kvq_pool *pool, const void
 tc_status tc_kvq_read(const tc_plan *plan, const tc_kvq_pool *pool, int32_t seq, void *k_out, void *v_out, void *stream);
 
 /* tc_mixed_attention over a cache in 8 bits: the same softmax over the numbers that the cache stands for, with the
- * same accumulation and roundings. */
+ * same accumulation and roundings.  A key or value that is NaN reaches the rows that attend over its token, and no others. */
 tc_status tc_kvq_mixed_attention(const tc_plan *plan, const tc_kvq_pool *pool, const void *q, void *out, float scale,
                                  void *workspace, size_t workspace_bytes, void *stream);
 

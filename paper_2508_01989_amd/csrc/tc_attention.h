@@ -68,6 +68,10 @@ __device__ __forceinline__ float scale_of(int exponent_byte) { return __uint_as_
 // Bytes t of a word that hold tokens below `n` (the four tokens of a word are consecutive): the others become zero.
 __device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u; }
 
+// Where the word of V lies that holds tokens 4 g .. 4 g + 3 of element d, in bytes inside a (block, KV head) tile in 8 bits.
+template <int D>
+__device__ __forceinline__ int v8_word(int g, int d) { return (((d >> 4) & 1) * 64 + g * 16 + (d & 15)) * (D / 8) + (d >> 5) * 4; }
+
 struct AttnArgs {
     uint16_t *k_pool, *v_pool;  // written only by the variant that also stores the batch's new rows
     uint8_t *scales;            // a cache in 8 bits: [block][KV head][2], the exponents of its K and V scales
@@ -386,7 +390,8 @@ struct PrefillLds<D, NW, true> {
     static constexpr int kRaw = kV + kStagesV * C::kTileBytes;
     static constexpr int kIds = kRaw + NW * kRawStages * kRawPage;
     static constexpr int kSlots = 1 + kRawStages;  // of a wave
-    static constexpr int kBytes = kIds + NW * kSlots * 64 * 4;
+    static constexpr int kFlags = kIds + NW * kSlots * 64 * 4;  // one int a wave: it has put zeros in the place of NaN (see TileWidener)
+    static constexpr int kBytes = kFlags + NW * 4;
     static_assert(NW == kMixedWaves, "a wave for each tensor of the four pages of a tile");
     static_assert(decode_lds_bytes(NW, 16, D) <= (size_t)kIds && kBytes <= 160 * 1024);
 };
@@ -490,6 +495,9 @@ __device__ __forceinline__ void barrier_lds() {
     asm volatile("" ::: "memory");
 }
 
+// The top bit of every byte of a word that is NaN (E4M3: all exponent and mantissa bits set).
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
+
 // A cache in 8 bits: wave w of the eight moves page w mod 4 of every tile, K (w < 4) or V^T, in two steps.  fetch() copies the page as it
 // lies in the pool into a stage of the wave's own, with direct-to-LDS loads, and beside it the exponent of its scale;
 // widen() reads it back a step or more later and leaves it in the tile's stage in 16 bits, in the layout that the sweep reads.  A byte is
@@ -505,6 +513,7 @@ struct TileWidener {
     typedef __attribute__((address_space(3))) void *lptr_t;
     const uint8_t *src, *scales;  // pool + this lane's offset inside a (page, KV head) block; this head's exponent of block 0
     char *raw, *slots;            // this wave's stages and slots
+    int *flag;                    // this wave's
     char *dst;                    // this wave's page in stage 0 of its tensor
     int64_t page_stride;          // bytes per page (all KV heads)
     int scale_stride;
@@ -519,6 +528,7 @@ struct TileWidener {
         scales = A.scales + kvh * 2 + (is_v ? 1 : 0);
         raw = lds + L::kRaw + wave * (L::kRawStages * L::kRawPage);
         slots = lds + L::kIds + wave * (L::kSlots * 256);
+        flag = reinterpret_cast<int *>(lds + L::kFlags) + wave;
         dst = lds + (is_v ? L::kV : 0) + page_in_tile * C::kPageBytes;
     }
     __device__ __forceinline__ char *id_slot() const { return slots; }
@@ -528,8 +538,10 @@ struct TileWidener {
         __builtin_amdgcn_global_load_lds((gptr_t)(scales + id * scale_stride), (lptr_t)(slots + (1 + stage) * 256), 1, 0, 0);
     }
     // The page in `stage`, whose loads have landed, into the 16-bit stage `tile_stage`; its first n_valid tokens are real.  Slots behind those hold
-    // undefined bytes: they get probability 0, but V must be finite for the MFMA, so zero.
-    __device__ __forceinline__ void widen(int stage, int tile_stage, int n_valid, int lane) const {
+    // undefined bytes: they get probability 0, but V must be finite for the MFMA, so zero.  So must be a token's V for the rows that do not
+    // attend over it yet (`diagonal`: the tile has such tokens): a NaN there becomes zero too, which is flagged, and the rows that do attend over it
+    // get theirs at the end of the sweep (restore_nan).
+    __device__ __forceinline__ void widen(int stage, int tile_stage, int n_valid, bool diagonal, int lane) const {
         const char *from = raw + stage * L::kRawPage;
         char *to = dst + tile_stage * C::kTileBytes;
         const float scale = scale_of(__builtin_amdgcn_readfirstlane((int)*reinterpret_cast<const uint8_t *>(slots + (1 + stage) * 256)));
@@ -559,6 +571,19 @@ struct TileWidener {
                     b[c] &= mb;
                 }
             }
+            if (diagonal) {
+                uint32_t any = 0;
+#pragma unroll
+                for (int c = 0; c < W; c++) any |= nan_bytes(a[c]) | nan_bytes(b[c]);
+                if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
+#pragma unroll
+                    for (int c = 0; c < W; c++) {
+                        a[c] &= ~((nan_bytes(a[c]) >> 7) * 255u);
+                        b[c] &= ~((nan_bytes(b[c]) >> 7) * 255u);
+                    }
+                    *flag = 1;
+                }
+            }
             char *at = to + (16 * half + j) * 32 + (g ^ (j >> 3)) * 16;
 #pragma unroll
             for (int c = 0; c < W; c++) *reinterpret_cast<typename E::x8 *>(at + c * 1024) = E::widen8(a[c], b[c], scale);
@@ -567,6 +592,30 @@ struct TileWidener {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 };
+
+// Rare: the sweep of a prefill item, over tokens up to `end`, met NaN among the V of tokens from `first` on, which not all rows attend over, and put
+// zeros there.  The whole workgroup finds the first such token of every element, and the accumulators of the rows that attend over it become NaN.
+// A lane's row is position p_abs; its accumulators are as in PiecePartial.
+template <int D>
+__device__ __forceinline__ void restore_nan(const AttnArgs &A, const int32_t *__restrict__ pages, int kvh, int first, int end, int p_abs, int hh, int *lds, int tid, int T,
+                                            f32x16 (&o)[D / 32]) {
+    __syncthreads();  // every wave has left the sweep
+    for (int d = tid; d < D; d += T) lds[d] = INT32_MAX;
+    __syncthreads();
+    for (int x = tid; x < (end - first + 3) / 4 * D; x += T) {  // four tokens of one element (`first` begins a tile)
+        const int d = x % D, tok = first + x / D * 4, g = (tok % kBlock) / 4;
+        const uint8_t *tile = reinterpret_cast<const uint8_t *>(A.v_pool) + ((int64_t)pages[tok / kBlock] * A.Hkv + kvh) * (kBlock * D);
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(tile + v8_word<D>(g, d)) & first_bytes(end - tok);
+        if (const uint32_t bad = nan_bytes(w)) atomicMin(lds + d, tok + (__ffs((int)bad) - 1) / 8);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < D / 32; c++)
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+            if (lds[32 * c + 8 * (r >> 2) + 4 * hh + (r & 3)] <= p_abs) o[c][r] = __builtin_nanf("");
+    __syncthreads();  // the LDS is free
+}
 
 // max / sum across the two half-waves (lanes l and l ^ 32 hold the two halves of a row).
 __device__ __forceinline__ float half_swap_max(float v) {
@@ -754,6 +803,7 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
     // A cache in 8 bits: all waves fetch and widen.  Tile j of the sweep is fetched into raw stage j mod 2 (two steps ahead of its widening)
     // and widened into stage j mod 3 of both tensors in step j - 2; the first two before step 0.
     typedef std::conditional_t<KVQ, TileWidener<D, E>, int> Widener;
+    const auto diagonal = [&](int tile) { return (tile + 1) * C::kTileTokens > ctx + pos0 + 1; };  // has tokens that the item's first row does not attend over
     [[maybe_unused]] Widener wd = [&] {
         if constexpr (KVQ) return TileWidener<D, E>(A, kvh, lds, wave, lane);
         else return 0;
@@ -767,14 +817,15 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
     auto page_index = [&](int tile) { return min(tile * C::kTilePages + pg, n_pages - 1); };  // past the end: the last page, whose copy is never used
     if constexpr (KVQ) {
         const int32_t *ids = rec + RC_IDS + pg;
+        *wd.flag = 0;
         wd.fetch(ids[0], 0);
         wd.fetch(ids[C::kTilePages], 1);
         page_id_fetch(pages + page_index(t_begin + 4), wd.id_slot());
         wait_loads_but<TileWidener<D, E>::kLoads + 1>();
-        wd.widen(0, 0, kv_len - (t_begin * C::kTilePages + pg) * kBlock, lane);
+        wd.widen(0, 0, kv_len - (t_begin * C::kTilePages + pg) * kBlock, diagonal(t_begin), lane);
         wd.fetch(ids[2 * C::kTilePages], 0);
         wait_loads_but<TileWidener<D, E>::kLoads + 1>();
-        wd.widen(1, 1, kv_len - ((t_begin + 1) * C::kTilePages + pg) * kBlock, lane);
+        if (n_sweep > 1) wd.widen(1, 1, kv_len - ((t_begin + 1) * C::kTilePages + pg) * kBlock, diagonal(t_begin + 1), lane);
         wd.fetch(ids[3 * C::kTilePages], 1);
     } else if (copier) {
         // In the order in which the sweep needs them.  The ids of all these pages lie in the record, so that only two accesses to
@@ -890,7 +941,7 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
     auto copies = [&](int j) {  // K(j+NS) replaces K(j), V(j+VS-1) replaces V(j-1)
         const int vm1 = v0 == 0 ? VS - 1 : v0 - 1;
         if constexpr (KVQ) {  // tile j + 2 replaces tile j - 1
-            if (j + 2 < n_sweep) wd.widen(j & 1, vm1, kv_len - ((t_begin + j + 2) * C::kTilePages + pg) * kBlock, lane);
+            if (j + 2 < n_sweep) wd.widen(j & 1, vm1, kv_len - ((t_begin + j + 2) * C::kTilePages + pg) * kBlock, diagonal(t_begin + j + 2), lane);
             page_id_fetch(pages + page_index(t_begin + j + 5), wd.id_slot());
             wd.fetch(id_next[0], j & 1);
         } else if constexpr (NW == kMixedWaves) {
@@ -996,6 +1047,12 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
     if (copier) wait_all_loads();  // copies past the end of the range, before the LDS is used for anything else
 
     float l = half_swap_sum(l_run);
+    if constexpr (KVQ) {  // (a flag is set a barrier before the end of the sweep at least)
+        const int *flags = reinterpret_cast<const int *>(lds + L::kFlags);
+        if (__builtin_amdgcn_ballot_w64(lane < NW && flags[lane & (NW - 1)] != 0) != 0)
+            restore_nan<D>(A, pages, kvh, max(t_begin * C::kTileTokens, (ctx + pos0 + 1) / C::kTileTokens * C::kTileTokens), min(t_end * C::kTileTokens, kv_len), p_abs, hh,
+                           reinterpret_cast<int *>(lds), tid, NW * 64, o);
+    }
     if (NW == kMixedWaves && region >= 0) {  // (small workgroups run whole items only)
         // A piece of a cut item: every lane leaves its unnormalised accumulators, and the rows' running maximum
         // (log2 domain) and sum, in the piece's region of the workspace as they lie in registers; rows that see no

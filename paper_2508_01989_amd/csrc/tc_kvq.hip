@@ -38,10 +38,6 @@ __device__ __forceinline__ void transpose4(const uint32_t (&r)[4], uint32_t (&c)
     c[2] = __builtin_amdgcn_perm(hi23, hi01, 0x05040100);
     c[3] = __builtin_amdgcn_perm(hi23, hi01, 0x07060302);
 }
-// Where the word of V lies that holds tokens 4 g .. 4 g + 3 of element d, in bytes inside a (block, KV head) tile.
-template <int D>
-__device__ __forceinline__ int v8_word(int g, int d) { return (((d >> 4) & 1) * 64 + g * 16 + (d & 15)) * (D / 8) + (d >> 5) * 4; }
-
 // One tensor's exponent for a page, and how its rows are brought to it.
 template <class E>
 struct Quantiser {

@@ -220,3 +220,227 @@ def test_step_against_the_plain_form(tc, name, dtype):
     one.step()
     check_cache(one, after, "step again")
     assert np.array_equal(one.outputs(), got)
+
+
+SPECIAL = {
+    # NaN and infinities among the new rows: (shape, [(tensor, row, head, element)])
+    "chunk": ((8, 2, 128, [300, 1, 1], [70, 40, 500]), [("v", 5, 0, 3), ("v", 130, 1, 127), ("v", 131, 1, 127), ("k", 200, 0, 9), ("v", 299, 0, 64), ("v", 300, 1, 1)]),
+    "chunk_d64": ((4, 4, 64, [150, 1], [33, 10]), [("v", 0, 1, 63), ("k", 149, 2, 0), ("v", 77, 3, 31)]),
+    "first_chunk": ((16, 1, 128, [65], [0]), [("v", 64, 0, 5), ("v", 63, 0, 6), ("v", 0, 0, 7)]),
+    "cut_chunk": ((8, 2, 128, [77], [1500]), [("v", 76, 0, 100), ("v", 1, 1, 0), ("k", 60, 1, 0)]),
+    "levelled_chunk": ((32, 8, 128, [700], [900]), [("v", 300, 3, 77), ("v", 699, 4, 0), ("k", 650, 7, 1)]),
+    "decodes": ((8, 2, 128, [1, 1, 1], [3, 1000, 64]), [("k", 0, 1, 5), ("v", 2, 0, 99)]),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("name", SPECIAL)
+def test_nan_reaches_the_rows_that_attend_over_it_and_no_others(tc, name, dtype):
+    shape, marks = SPECIAL[name]
+    c = Case(name, *shape, dtype=dtype)
+    inf, nan = (0x7C00, 0x7E01) if dtype == "fp16" else (0x7F80, 0x7FC1)
+    for i, (x, row, head, d) in enumerate(marks):
+        (c.k_new if x == "k" else c.v_new)[row, head, d] = (inf, nan, inf | 0x8000)[i % 3]
+    print(f"[case] special {name} {dtype}", flush=True)
+    cache = c.oracle_cache()
+    dev = Device(tc, c)
+    dev.step()
+    check_cache(dev, cache, name)
+    want, bound = c.attention(cache)
+    assert np.isnan(want).any() and np.isfinite(want).any()
+    check_attention(dev.outputs(), want, bound, name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_every_pattern_is_quantised_and_read_back(tc, dtype):
+    """All 65536 patterns of the type, in blocks of their own and one by one into blocks whose scale then grows, at both ends of the range."""
+    u = np.arange(65536, dtype=np.uint16)
+    rng = np.random.default_rng(7)
+    c = Case("patterns", 4, 2, 64, [512, 512, 1, 1, 1], [0, 0, 0, 1, 2], dtype=dtype)
+    c.k_new[:512], c.v_new[:512] = u.reshape(512, 2, 64), u[::-1].reshape(512, 2, 64)  # neighbours share a block
+    c.k_new[512:1024], c.v_new[512:1024] = rng.permutation(u).reshape(512, 2, 64), rng.permutation(u).reshape(512, 2, 64)
+    big, small = (0x7BFF, 0x0001) if dtype == "fp16" else (0x7F7F, 0x0001)
+    c.k_hist[:], c.v_hist[:] = small, 0x0400
+    c.k_new[1024:], c.v_new[1024:] = big, 0x8000 | big
+    print(f"[case] patterns {dtype}", flush=True)
+    cache = c.oracle_cache()
+    dev = Device(tc, c)
+    dev.append()
+    check_cache(dev, cache, dtype)
+    for s in range(c.S):
+        for x, y in zip(dev.read(s), cache.read(c.table[s], int(c.kv[s]))):
+            assert np.array_equal(x, y, equal_nan=True)
+
+
+def test_blocks_beyond_two_and_four_gigabytes(tc):
+    """The same batch at the far end of pools of 4.5 GB each: byte offsets pass 32 bits."""
+    import torch
+    c = Case("far", 16, 8, 128, [70, 1, 1], [100, 1300, 17])
+    cache = c.oracle_cache()
+    want, bound = c.attention(cache)
+    far = 275000  # blocks before this batch's, 16 KiB each
+    near = Device(tc, c)
+    near.step()
+    n = c.Hkv * 16 * c.D
+    k = torch.zeros((far + c.blocks) * n, dtype=torch.uint8, device="cuda:0")
+    v = torch.zeros_like(k)
+    s = torch.zeros((far + c.blocks) * c.Hkv * 2, dtype=torch.uint8, device="cuda:0")
+    fresh = Device(tc, c)
+    k[far * n:], v[far * n:], s[far * c.Hkv * 2:] = fresh.k, fresh.v, fresh.scales
+    pool = tc.make_kvq_pool(c.Hq, c.Hkv, c.D, far + c.blocks, k, v, s)
+    plan = tc.Plan(pool, c.q_start, c.ctx, c.table + far)
+    print("[case] far blocks", flush=True)
+    tc.tc_kvq_mixed_attention_append(plan, pool, fresh.q, fresh.k_new, fresh.v_new, fresh.out, c.scale, fresh.workspace)
+    out = fresh.outputs()
+    assert np.array_equal(out, near.outputs())
+    check_attention(out, want, bound, "far")
+    assert torch.equal(k[far * n:], near.k) and torch.equal(v[far * n:], near.v) and torch.equal(s[far * c.Hkv * 2:], near.scales)
+    assert not k[:far * n].any() and not v[:far * n].any() and not s[:far * c.Hkv * 2].any()
+    n_tok = int(c.kv[1])
+    ko = torch.empty((n_tok, c.Hkv, c.D), dtype=torch.int16, device="cuda:0")
+    vo = torch.empty_like(ko)
+    tc.tc_kvq_read(plan, pool, 1, ko, vo)
+    torch.cuda.synchronize()
+    for x, y in zip((ko, vo), cache.read(c.table[1], n_tok)):
+        assert np.array_equal(kvq.widen(x.cpu().numpy().view(np.uint16), "bf16"), y)
+
+
+def test_generation_over_one_plan_object(tc):
+    """As a serving loop runs it: prompts in two chunks of odd lengths, then token by token beside each other, one plan object updated for every
+    iteration; then the requests move into other blocks (read, append) and go on.  Cache and outputs of every iteration."""
+    import torch
+    rng = np.random.default_rng(11)
+    Hq, Hkv, D, lens, steps = 8, 2, 128, [45, 97], 20
+    total = [n + steps + 3 for n in lens]
+    blocks = 40
+    ids = rng.permutation(blocks).astype(np.int32)
+    width = -(-max(total) // 16)
+    table, table2 = ids[:2 * width].reshape(2, width), ids[2 * width:4 * width].reshape(2, width)
+    rows = lambda n, h: bits_of(rng.standard_normal((n, h, D), np.float32) * np.exp2(rng.integers(-6, 3, (n, h, 1))).astype(np.float32), "bf16")  # noqa: E731
+    q, k, v = ([rows(n, h) for n in total] for h in (Hq, Hkv, Hkv))
+    cache = kvq.Cache(blocks, Hkv, D)
+    dk, dv = (torch.full((blocks * Hkv * 16 * D,), 0x7F, dtype=torch.uint8, device="cuda:0") for _ in range(2))
+    ds = torch.full((blocks * Hkv * 2,), 0xFF, dtype=torch.uint8, device="cuda:0")
+    pool = tc.make_kvq_pool(Hq, Hkv, D, blocks, dk, dv, ds)
+    up = lambda x: torch.from_numpy(np.concatenate(x).view(np.int16)).to("cuda:0")  # noqa: E731
+    done, plan, scale = [0, 0], None, float(np.float32(D ** -0.5))
+
+    def iterate(seqs, counts, tab):
+        nonlocal plan
+        q_start = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        ctx = np.array([done[s] for s in seqs], np.int32)
+        tab = np.ascontiguousarray(tab[seqs])
+        part = lambda x: [x[s][done[s]:done[s] + n] for s, n in zip(seqs, counts)]  # noqa: E731
+        if plan is None:
+            plan = tc.Plan(pool, q_start, ctx, tab)
+        else:
+            plan.update(pool, q_start, ctx, tab)
+        ws = torch.empty(max(16, plan.workspace_bytes), dtype=torch.uint8, device="cuda:0")
+        out = torch.empty((int(q_start[-1]), Hq, D), dtype=torch.int16, device="cuda:0")
+        tc.tc_kvq_mixed_attention_append(plan, pool, up(part(q)), up(part(k)), up(part(v)), out, scale, ws)
+        torch.cuda.synchronize()
+        cache.append(q_start, ctx, tab, np.concatenate(part(k)), np.concatenate(part(v)))
+        kp, vp = cache.widened_pools(tab, ctx + counts)
+        args = (Hq, Hkv, D, 16, q_start, ctx, tab, np.concatenate(part(q)), scale)
+        want, mean = oracle.attention(kp, vp, *args), oracle.attention(kp, vp & np.uint16(0x7FFF), *args)
+        check_attention(kvq.widen(out.cpu().numpy().view(np.uint16), "bf16"), want, HALF_STEP["bf16"] * 1.02 * (mean + np.abs(want)) + 1e-30, f"at {done}")
+        for s, n in zip(seqs, counts):
+            done[s] += n
+
+    def same_cache():
+        for x, y in ((dk, cache.k), (dv, cache.v), (ds, cache.scales)):
+            assert np.array_equal(x.cpu().numpy().reshape(y.shape), y)
+
+    print("[case] generation", flush=True)
+    iterate([0], [30], table)
+    iterate([0, 1], [15, 50], table)
+    iterate([1], [47], table)
+    for _ in range(steps):
+        iterate([0, 1], [1, 1], table)
+    same_cache()
+    plan.update(pool, np.array([0, 1, 2], np.int32), np.array(done, np.int32) - 1, table)
+    n = sum(done)
+    ko = torch.empty((n, Hkv, D), dtype=torch.int16, device="cuda:0")
+    vo = torch.empty_like(ko)
+    tc.tc_kvq_read(plan, pool, -1, ko, vo)
+    q_start = np.concatenate([[0], np.cumsum(done)]).astype(np.int32)
+    plan.update(pool, q_start, np.zeros(2, np.int32), table2)
+    tc.tc_kvq_append(plan, pool, ko, vo)
+    torch.cuda.synchronize()
+    was = [cache.read(table[s], done[s]) for s in range(2)]
+    cache.append(q_start, np.zeros(2, np.int32), table2, ko.cpu().numpy().view(np.uint16), vo.cpu().numpy().view(np.uint16))
+    for s in range(2):
+        for x, y in zip(was[s], cache.read(table2[s], done[s])):
+            assert np.array_equal(x, y)
+    same_cache()
+    for _ in range(3):
+        iterate([1, 0], [1, 1], table2)
+    same_cache()
+
+
+@pytest.mark.parametrize("name", ["decodes_ragged", "many_decodes_by_single_waves", "chunk_and_decodes", "queue", "long_decode_many_partials"])
+def test_step_captured_in_a_graph_and_on_another_stream(tc, name):
+    import torch
+    c = Case(name, *SHAPES[name])
+    eager = Device(tc, c)
+    eager.step()
+    want, (k, v, s) = eager.outputs(), eager.cache()
+    print(f"[case] graph {name}", flush=True)
+    stream = torch.cuda.Stream()
+    dev = Device(tc, c, stream=stream)
+    with torch.cuda.stream(stream):
+        dev.step()
+    stream.synchronize()
+    assert np.array_equal(dev.outputs(), want)
+    fresh = [x.clone() for x in (dev.k, dev.v, dev.scales)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        dev.step()
+    torch.cuda.synchronize()
+    for i in range(4):
+        dev.out.zero_()
+        dev.out[-1] = -1
+        eager.step()  # eager work of the same kernels between the replays
+        graph.replay()
+        assert np.array_equal(dev.outputs(), want), f"replay {i}"
+        for x, y in zip(fresh, (dev.k, dev.v, dev.scales)):
+            assert torch.equal(x, y)
+        assert np.array_equal(eager.outputs(), want)
+    for x, y in zip(dev.cache(), (k, v, s)):
+        assert np.array_equal(x, y)
+
+
+def test_two_calls_at_once_on_two_streams(tc):
+    """Plans, workspaces and caches of their own: nothing is shared."""
+    import torch
+    cases = [Case(n, *SHAPES[n]) for n in ("queue", "decodes_ragged")]
+    alone = []
+    for c in cases:
+        d = Device(tc, c)
+        d.step()
+        alone.append((d.outputs(), d.cache()))
+    streams = [torch.cuda.Stream() for _ in cases]
+    devs = [Device(tc, c, stream=s) for c, s in zip(cases, streams)]
+    print("[case] two streams", flush=True)
+    for _ in range(6):
+        for d in devs:
+            d.step()
+    for d, (out, cache) in zip(devs, alone):
+        assert np.array_equal(d.outputs(), out)
+        for x, y in zip(d.cache(), cache):
+            assert np.array_equal(x, y)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(257, 257, 64), (1024, 1024, 64), (130, 130, 128)])
+def test_many_kv_heads(tc, Hq, Hkv, D):
+    """More KV heads than compute units, and a number that no workgroup's waves divide."""
+    c = Case("heads", Hq, Hkv, D, [20, 1, 1], [7, 33, 100], spread=1)
+    cache = c.oracle_cache()
+    print(f"[case] {Hkv} heads", flush=True)
+    dev = Device(tc, c)
+    dev.step()
+    check_cache(dev, cache, "heads")
+    check_attention(dev.outputs(), *c.attention(cache), "heads")
+    for s in range(c.S):
+        for x, y in zip(dev.read(s), cache.read(c.table[s], int(c.kv[s]))):
+            assert np.array_equal(x, y)
