@@ -249,7 +249,7 @@ tc_status tc_kvq_mixed_attention(const tc_plan *plan, const tc_kvq_pool *pool, c
     tc_status st = check_kvq(plan, pool);
     if (st != TC_OK || plan->T == 0) return st;
     if ((st = check_kvq_attention(plan, q, out, scale, workspace, workspace_bytes)) != TC_OK || (st = check_kvq_device(plan)) != TC_OK) return st;
-    return device_result(tc::launch_kvq_attention(plan, pool, q, out, scale, workspace, stream), "tc_kvq_mixed_attention launch");
+    return device_result(tc::launch_kvq_attention(plan, pool, q, nullptr, nullptr, out, scale, workspace, stream), "tc_kvq_mixed_attention launch");
 }
 
 tc_status tc_kvq_mixed_attention_append(const tc_plan *plan, const tc_kvq_pool *pool, const void *q, const void *k_new, const void *v_new,
@@ -258,9 +258,12 @@ tc_status tc_kvq_mixed_attention_append(const tc_plan *plan, const tc_kvq_pool *
     if (st != TC_OK || plan->T == 0) return st;
     if ((st = check_kvq_rows(k_new, v_new)) != TC_OK) return st;
     if ((st = check_kvq_attention(plan, q, out, scale, workspace, workspace_bytes)) != TC_OK || (st = check_kvq_device(plan)) != TC_OK) return st;
-    st = device_result(tc::launch_kvq_append(plan, pool, k_new, v_new, stream), "tc_kvq_mixed_attention_append launch");
-    if (st != TC_OK) return st;
-    return device_result(tc::launch_kvq_attention(plan, pool, q, out, scale, workspace, stream), "tc_kvq_mixed_attention_append launch");
+    // As in tc_mixed_attention_append: a batch of decodes is one launch, the rows of a chunk are stored first.
+    if (plan->n_pieces > 0) {
+        st = device_result(tc::launch_kvq_append(plan, pool, k_new, v_new, stream), "tc_kvq_mixed_attention_append launch");
+        if (st != TC_OK) return st;
+    }
+    return device_result(tc::launch_kvq_attention(plan, pool, q, k_new, v_new, out, scale, workspace, stream), "tc_kvq_mixed_attention_append launch");
 }
 
 }  // extern "C"

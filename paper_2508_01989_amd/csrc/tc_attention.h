@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "tc_internal.h"
+#include "tc_kvq_device.h"
 
 namespace tc {
 
@@ -30,8 +31,9 @@ struct Bf16 {
         typedef short s4 __attribute__((ext_vector_type(4)));
         return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s4, a), __builtin_bit_cast(s4, b), c, 0, 0, 0);
     }
-    // two E4M3 bytes times a power of two (HI: the upper two), in one instruction
+    // two E4M3 bytes times a power of two, and two elements over one as bytes (HI: the upper two), in one instruction
     template <bool HI> static __device__ __forceinline__ x2 widen2(uint32_t w, float scale) { return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI); }
+    template <bool HI> static __device__ __forceinline__ s16x2 narrow2(s16x2 old, x2 v, float scale) { return __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(old, v, scale, HI); }
 };
 struct Fp16 {
     static constexpr bool kKvq = false;
@@ -42,35 +44,14 @@ struct Fp16 {
     static __device__ __forceinline__ f32x16_t mfma32(x8 a, x8 b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ f32x4_t mfma16(x8 a, x8 b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ f32x4_t mfma16k16(x4 a, x4 b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0); }
-    // two E4M3 bytes times a power of two (HI: the upper two), in one instruction
+    // two E4M3 bytes times a power of two, and two elements over one as bytes (HI: the upper two), in one instruction
     template <bool HI> static __device__ __forceinline__ x2 widen2(uint32_t w, float scale) { return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, HI); }
+    template <bool HI> static __device__ __forceinline__ s16x2 narrow2(s16x2 old, x2 v, float scale) { return __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(old, v, scale, HI); }
 };
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-// The same types over a cache in 8 bits (tc_kvq_pool): bytes times the power of two of their block and KV head are exact in
-// either type, so they are widened on their way to the matrix cores and everything behind that is as above.
-template <class Base>
-struct KvE4m3 : Base {
-    static constexpr bool kKvq = true;
-    static __device__ __forceinline__ typename Base::x4 widen4(uint32_t w, float scale) {
-        const auto a = Base::template widen2<false>(w, scale), b = Base::template widen2<true>(w, scale);
-        return typename Base::x4{a[0], a[1], b[0], b[1]};
-    }
-    static __device__ __forceinline__ typename Base::x8 widen8(uint32_t lo, uint32_t hi, float scale) {
-        const auto a = widen4(lo, scale), b = widen4(hi, scale);
-        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-    }
-};
-__device__ __forceinline__ float scale_of(int exponent_byte) { return __uint_as_float((uint32_t)exponent_byte << 23); }
-// Bytes t of a word that hold tokens below `n` (the four tokens of a word are consecutive): the others become zero.
-__device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u; }
-
-// Where the word of V lies that holds tokens 4 g .. 4 g + 3 of element d, in bytes inside a (block, KV head) tile in 8 bits.
-template <int D>
-__device__ __forceinline__ int v8_word(int g, int d) { return (((d >> 4) & 1) * 64 + g * 16 + (d & 15)) * (D / 8) + (d >> 5) * 4; }
 
 struct AttnArgs {
     uint16_t *k_pool, *v_pool;  // written only by the variant that also stores the batch's new rows
@@ -494,9 +475,6 @@ __device__ __forceinline__ void barrier_lds() {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
-
-// The top bit of every byte of a word that is NaN (E4M3: all exponent and mantissa bits set).
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 
 // A cache in 8 bits: wave w of the eight moves page w mod 4 of every tile, K (w < 4) or V^T, in two steps.  fetch() copies the page as it
 // lies in the pool into a stage of the wave's own, with direct-to-LDS loads, and beside it the exponent of its scale;
@@ -1149,6 +1127,76 @@ __device__ __forceinline__ void decode_take_new_token(const AttnArgs &A, int kvh
     }
 }
 
+// The same for a cache in 8 bits, where the new row may also change the page's scales, and its older rows with them: no other workgroup may store it
+// while this one reads the page, so the wavefront always does.  It quantises the row as kvq_append_kernel does and stores what has changed: the
+// row's 16-byte pieces of K, the 16-byte pieces of V that hold its bytes, all older rows where a scale grows (rare), and the exponents.
+template <int D, class E>
+__device__ __forceinline__ void decode_take_new_token(const AttnArgs &A, int kvh, int qrow, int id, int tn, int j, int g, int &exponents, DecodePage8<D> &st) {
+    const int64_t src = ((int64_t)qrow * A.Hkv + kvh) * D, pair = (int64_t)id * A.Hkv + kvh;
+    const uint16_t *kn = A.k_new + src, *vn = A.v_new + src;
+    const bool has_k = j == tn, has_v = g == (tn >> 2);
+    uint32_t kw[D / 8] = {}, vw[D / 32] = {};  // 16 elements d = 16 (4 i + g) .. for each piece of K; d = 32 c + j and 32 c + 16 + j for each word of V
+    if (has_k) {
+#pragma unroll
+        for (int i = 0; i < D / 64; i++) {
+            const u32x4 *p = reinterpret_cast<const u32x4 *>(kn + (4 * i + g) * 16);
+            const u32x4 a = p[0], b = p[1];
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+                kw[8 * i + x] = a[x];
+                kw[8 * i + 4 + x] = b[x];
+            }
+        }
+    }
+    if (has_v) {
+#pragma unroll
+        for (int c = 0; c < D / 32; c++) vw[c] = (uint32_t)vn[32 * c + j] | (uint32_t)vn[32 * c + 16 + j] << 16;
+    }
+    Quantiser<E> qk(0, 0, 0), qv(0, 0, 0);
+    page_quantisers<E>(kw, vw, exponents, tn > 0, qk, qv);
+    exponents = (qk.e + 127) | (qv.e + 127) << 8;
+    if (qk.grows && j < tn) {
+#pragma unroll
+        for (int i = 0; i < D / 64; i++)
+#pragma unroll
+            for (int x = 0; x < 4; x++) st.k[i][x] = rescale_bytes(st.k[i][x], qk.shrink);
+    }
+    if (has_k) {
+#pragma unroll
+        for (int i = 0; i < D / 64; i++)
+#pragma unroll
+            for (int x = 0; x < 4; x++) st.k[i][x] = qk.bytes(kw[8 * i + 2 * x], kw[8 * i + 2 * x + 1]);
+    }
+    if (qv.grows && 4 * g < tn) {
+        const uint32_t is_old = first_bytes(tn - 4 * g);
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+#pragma unroll
+            for (int c = 0; c < D / 32; c++) st.v[i][c] = (rescale_bytes(st.v[i][c], qv.shrink) & is_old) | (st.v[i][c] & ~is_old);
+    }
+    if (has_v) {
+        const int at = 8 * (tn & 3);
+        const uint32_t keep = ~(0xFFu << at);
+#pragma unroll
+        for (int c = 0; c < D / 32; c++) {
+            const uint32_t w = qv.bytes(vw[c], 0);
+            st.v[0][c] = (st.v[0][c] & keep) | (w & 0xFF) << at;
+            st.v[1][c] = (st.v[1][c] & keep) | ((w >> 8) & 0xFF) << at;
+        }
+    }
+    uint8_t *kb = reinterpret_cast<uint8_t *>(A.k_pool) + pair * (kBlock * D) + (g * kBlock + j) * 16;
+    uint8_t *vb = reinterpret_cast<uint8_t *>(A.v_pool) + pair * (kBlock * D) + (g * kBlock + j) * (D / 8);
+    if (has_k || (qk.grows && j < tn)) {
+#pragma unroll
+        for (int i = 0; i < D / 64; i++) *reinterpret_cast<u32x4 *>(kb + i * 1024) = st.k[i];
+    }
+    if (has_v || (qv.grows && 4 * g < tn)) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) *reinterpret_cast<typename DecodePage8<D>::piece *>(vb + i * (8 * D)) = st.v[i];
+    }
+    if (j == 0 && g == 0) *reinterpret_cast<uint16_t *>(A.scales + 2 * pair) = (uint16_t)exponents;
+}
+
 // The append of decode rows: thread = (sequence, KV head, element), so that the lanes of a wave store adjacent rows of
 // the token-minor V block (four lanes per 128-byte line; with a thread per 8-element piece every lane of a store had a
 // line of its own and a workgroup took 5 us more).  kAppendPerThread elements per thread, all loads before the stores.
@@ -1303,7 +1351,8 @@ __device__ __forceinline__ void decode_sweep(const AttnArgs &A, int kvh, int qro
     constexpr int KS = D / 32;  // k-steps of K Q^T
     const int j = lane & 15, g = lane >> 4;
     const int G = A.G;
-    const int my_page = pages[min(lane, n_pg - 1)];  // lane i holds the id of page i of the range
+    // lane i holds the id of page i of the range (a cache in 8 bits: its last page's, then those of the others)
+    const int my_page = pages[E::kKvq ? (lane == 0 ? n_pg - 1 : min(lane - 1, n_pg - 1)) : min(lane, n_pg - 1)];
     int my_scales = 0;                               // and the exponents of its scales
     if constexpr (E::kKvq) my_scales = *reinterpret_cast<const uint16_t *>(A.scales + ((int64_t)my_page * A.Hkv + kvh) * 2);
 
@@ -1321,21 +1370,26 @@ __device__ __forceinline__ void decode_sweep(const AttnArgs &A, int kvh, int qro
     // i+1 .. i+NS-1 are in flight.
     DecodePageOf<D, E> st[NS];
     if constexpr (E::kKvq) {
-        // Every step of the loop fetches, so that the compiler's count of the loads in flight is exact (see below): its last turn may fetch up to NS - 1 pages that no
-        // step consumes, which are the range's last one again (lanes past it hold that), out of L2.
+        // The last page first (lane 0 holds its id): it alone may be partial, and it is the one that the sequence's new token goes into, which costs no page of
+        // the stream behind it its place in the ring.  Every step of the loop fetches, so that the compiler's count of the loads in flight is exact (see below): its last turn
+        // may fetch up to NS - 1 pages that no step consumes, a page of the range again, out of L2.
 #pragma unroll
-        for (int u = 0; u < NS - 1; u++) decode_fetch<D>(A, kvh, __builtin_amdgcn_readlane(my_page, u), j, g, st[u]);
-        int at = 0;
+        for (int u = 0; u < NS; u++) decode_fetch<D>(A, kvh, __builtin_amdgcn_readlane(my_page, u), j, g, st[u]);
+        int exponents = __builtin_amdgcn_readlane(my_scales, 0);
+        if (takes_new)
+            decode_take_new_token<D, E>(A, kvh, qrow, __builtin_amdgcn_readlane(my_page, 0), (n_tok - 1) & (kBlock - 1), j, g, exponents, st[0]);
+        decode_consume<D, E>(A, st[0], exponents, qreg, n_tok - (n_pg - 1) * kBlock, g, o, m_run, l_run);
+        int at = 1;
         for (; at + NS <= n_pg; at += NS) {
 #pragma unroll
             for (int u = 0; u < NS; u++) {
-                decode_fetch<D>(A, kvh, __builtin_amdgcn_readlane(my_page, (at + u + NS - 1) & 63), j, g, st[(u + NS - 1) % NS]);
-                decode_consume<D, E>(A, st[u], __builtin_amdgcn_readlane(my_scales, at + u), qreg, n_tok - (at + u) * kBlock, g, o, m_run, l_run);
+                decode_fetch<D>(A, kvh, __builtin_amdgcn_readlane(my_page, (at + u + NS - 1) & 63), j, g, st[u]);
+                decode_consume<D, E>(A, st[(u + 1) % NS], __builtin_amdgcn_readlane(my_scales, at + u), qreg, kBlock, g, o, m_run, l_run);
             }
         }
 #pragma unroll
         for (int u = 0; u < NS - 1; u++)
-            if (at + u < n_pg) decode_consume<D, E>(A, st[u], __builtin_amdgcn_readlane(my_scales, at + u), qreg, n_tok - (at + u) * kBlock, g, o, m_run, l_run);
+            if (at + u < n_pg) decode_consume<D, E>(A, st[(u + 1) % NS], __builtin_amdgcn_readlane(my_scales, at + u), qreg, kBlock, g, o, m_run, l_run);
     } else {
 #pragma unroll
         for (int u = 0; u < NS - 1; u++)
@@ -1399,7 +1453,8 @@ struct WaveResults {
 // members leave their (m, l, O) in LDS and the team's first wave combines them, in wave order, with its
 // own and writes the output rows, or one partial result if the (sequence, KV head) has more teams (then
 // the team is the whole workgroup).
-template <int D, class E, int NS>
+// TAKE: the launch may be one that stores the batch's new rows.
+template <int D, class E, int NS, bool TAKE = true>
 __device__ __forceinline__ void decode_item(const AttnArgs &A, const int32_t *__restrict__ it, float *team_lds, int wg_waves) {
     using x4 = typename E::x4;
     using el = typename E::t;
@@ -1412,7 +1467,7 @@ __device__ __forceinline__ void decode_item(const AttnArgs &A, const int32_t *__
     const int kvh = it[DC_KVH], t0 = it[DC_BEGIN], t1 = it[DC_END], qrow = it[DC_QROW], slot = it[DC_SLOT];
     const int team_n = it[DC_TEAM] & 15, team_pos = (it[DC_TEAM] >> 4) & 7, merge_item = (it[DC_TEAM] >> 8) - 1;
     // the split ends with the sequence's newest token and this launch is the one that stores it
-    const bool takes_new = (it[DC_TEAM] & kTeamTailBit) && A.k_new != nullptr;
+    const bool takes_new = TAKE && (it[DC_TEAM] & kTeamTailBit) && A.k_new != nullptr;
     const int G = A.G;
     const int n_tok = t1 - t0;  // 0: a padding item, which only takes part in the barrier
 
@@ -1533,7 +1588,7 @@ __device__ __forceinline__ void wide_combine(const AttnArgs &A, const WaveResult
 // combination is spread over all threads.
 // W = 2: two splits (items it[0], it[1]) to a workgroup, R / 2 waves each: the two halves of up to 2048 tokens of one (sequence, KV head),
 // a team with one result, or splits of two pairs that are not cut (or one and a padding item).
-template <int D, class E, int NS, int R, int W, bool STORE>
+template <int D, class E, int NS, int R, int W, bool STORE, bool TAKE = true>
 __device__ __forceinline__ void decode_item_wide(const AttnArgs &A, const int32_t *__restrict__ items, float *lds) {
     constexpr int MT = D / 16, RI = R / W;  // RI: waves of a split
     int tid = threadIdx.x;
@@ -1551,7 +1606,7 @@ __device__ __forceinline__ void decode_item_wide(const AttnArgs &A, const int32_
     for (int c = 0; c < MT; c++) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_run = -1e30f, l_run = 0.f;
     if (p1 > p0) {
-        const bool takes_new = p1 == n_pages && (team & kTeamTailBit) && A.k_new != nullptr;
+        const bool takes_new = TAKE && p1 == n_pages && (team & kTeamTailBit) && A.k_new != nullptr;
         decode_sweep<D, E, NS, STORE>(A, kvh, qrow, A.pages + it[DC_PAGEOFF] + t0 / kBlock + p0, p1 - p0, min(t1 - t0, p1 * kBlock) - p0 * kBlock,
                                takes_new, lane, o, m_run, l_run);
     }
@@ -1627,6 +1682,7 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == kMixedWaves ? 1 : CHUNK ?
     A.n_prefill = sc.n_prefill; A.n_decode = sc.n_decode; A.Hq = sc.Hq; A.Hkv = sc.Hkv; A.G = sc.G; A.fused = sc.fused; A.queue = sc.queue;
     A.scale_log2 = sc.scale_log2; A.scales = sc.scales;
     constexpr int NS = E::kKvq ? kDecodeStages8 : kDecodeStages;
+    constexpr bool TAKE = !(E::kKvq && CHUNK);
     if constexpr (!CHUNK && !E::kKvq) {
         const int first_append_wg = (int)gridDim.x - sc.n_front;
         if ((int)blockIdx.x >= first_append_wg) {
@@ -1654,8 +1710,8 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == kMixedWaves ? 1 : CHUNK ?
         const bool sweep = wg < A.n_prefill;
         const auto run = [&](int unit) __attribute__((always_inline)) {
             const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-            if constexpr (WIDE > 0) decode_item_wide<D, E, NS, WAVES, 1, false>(A, decode + (int64_t)unit * kItemInts, reinterpret_cast<float *>(lds));
-            else decode_item<D, E, NS>(A, decode + ((int64_t)unit * WAVES + wave) * kItemInts, reinterpret_cast<float *>(lds), WAVES);
+            if constexpr (WIDE > 0) decode_item_wide<D, E, NS, WAVES, 1, false, TAKE>(A, decode + (int64_t)unit * kItemInts, reinterpret_cast<float *>(lds));
+            else decode_item<D, E, NS, TAKE>(A, decode + ((int64_t)unit * WAVES + wave) * kItemInts, reinterpret_cast<float *>(lds), WAVES);
         };
         int first = wg - A.n_prefill;
         if (sc.n_drawers > 0) {
@@ -1722,8 +1778,8 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == kMixedWaves ? 1 : CHUNK ?
         const int idx = (wg - A.n_prefill) * WAVES + wave;
         // the decode items fill whole workgroups (padding items at the end of some): every wave gets one
         if constexpr (WIDE > 0)
-            decode_item_wide<D, E, NS, WAVES, WIDE, false>(A, decode + (int64_t)(wg - A.n_prefill) * WIDE * kItemInts, reinterpret_cast<float *>(lds));
-        else if (idx < A.n_decode) decode_item<D, E, NS>(A, decode + (int64_t)idx * kItemInts, reinterpret_cast<float *>(lds), WAVES);
+            decode_item_wide<D, E, NS, WAVES, WIDE, false, TAKE>(A, decode + (int64_t)(wg - A.n_prefill) * WIDE * kItemInts, reinterpret_cast<float *>(lds));
+        else if (idx < A.n_decode) decode_item<D, E, NS, TAKE>(A, decode + (int64_t)idx * kItemInts, reinterpret_cast<float *>(lds), WAVES);
     }
 #ifdef TC_WG_TRACE
     wg_trace(t_start, t_mid, (int)blockIdx.x >= sc.n_prefill);
