@@ -258,12 +258,13 @@ tc_status tc_kvq_mixed_attention_append(const tc_plan *plan, const tc_kvq_pool *
     if (st != TC_OK || plan->T == 0) return st;
     if ((st = check_kvq_rows(k_new, v_new)) != TC_OK) return st;
     if ((st = check_kvq_attention(plan, q, out, scale, workspace, workspace_bytes)) != TC_OK || (st = check_kvq_device(plan)) != TC_OK) return st;
-    // As in tc_mixed_attention_append: a batch of decodes is one launch, the rows of a chunk are stored first.
-    if (plan->n_pieces > 0) {
+    const bool apart = tc::kvq_append_apart(plan);
+    if (apart) {
         st = device_result(tc::launch_kvq_append(plan, pool, k_new, v_new, stream), "tc_kvq_mixed_attention_append launch");
         if (st != TC_OK) return st;
     }
-    return device_result(tc::launch_kvq_attention(plan, pool, q, k_new, v_new, out, scale, workspace, stream), "tc_kvq_mixed_attention_append launch");
+    return device_result(tc::launch_kvq_attention(plan, pool, q, apart ? nullptr : k_new, apart ? nullptr : v_new, out, scale, workspace, stream),
+                         "tc_kvq_mixed_attention_append launch");
 }
 
 }  // extern "C"

@@ -1130,28 +1130,47 @@ __device__ __forceinline__ void decode_take_new_token(const AttnArgs &A, int kvh
 // The same for a cache in 8 bits, where the new row may also change the page's scales, and its older rows with them: no other workgroup may store it
 // while this one reads the page, so the wavefront always does.  It quantises the row as kvq_append_kernel does and stores what has changed: the
 // row's 16-byte pieces of K, the 16-byte pieces of V that hold its bytes, all older rows where a scale grows (rare), and the exponents.
-template <int D, class E>
-__device__ __forceinline__ void decode_take_new_token(const AttnArgs &A, int kvh, int qrow, int id, int tn, int j, int g, int &exponents, DecodePage8<D> &st) {
-    const int64_t src = ((int64_t)qrow * A.Hkv + kvh) * D, pair = (int64_t)id * A.Hkv + kvh;
-    const uint16_t *kn = A.k_new + src, *vn = A.v_new + src;
-    const bool has_k = j == tn, has_v = g == (tn >> 2);
-    uint32_t kw[D / 8] = {}, vw[D / 32] = {};  // 16 elements d = 16 (4 i + g) .. for each piece of K; d = 32 c + j and 32 c + 16 + j for each word of V
-    if (has_k) {
+// The row is requested before the pages of the ring: loads complete in order, and behind them it would have the wave wait for all of those.
+template <int D>
+struct NewToken8 {
+    uint32_t kw[D / 8], v[D / 16];  // 16 elements d = 16 (4 i + g) .. for each piece of K; d = 16 c + j for each byte of V
+    __device__ __forceinline__ void load(const AttnArgs &A, int kvh, int qrow, int tn, int j, int g) {
+        const int64_t src = ((int64_t)qrow * A.Hkv + kvh) * D;
+        const uint16_t *kn = A.k_new + src, *vn = A.v_new + src;
 #pragma unroll
-        for (int i = 0; i < D / 64; i++) {
-            const u32x4 *p = reinterpret_cast<const u32x4 *>(kn + (4 * i + g) * 16);
-            const u32x4 a = p[0], b = p[1];
+        for (int i = 0; i < D / 8; i++) kw[i] = 0;
 #pragma unroll
-            for (int x = 0; x < 4; x++) {
-                kw[8 * i + x] = a[x];
-                kw[8 * i + 4 + x] = b[x];
+        for (int i = 0; i < D / 16; i++) v[i] = 0;
+        if (j == tn) {
+#pragma unroll
+            for (int i = 0; i < D / 64; i++) {
+                const u32x4 *p = reinterpret_cast<const u32x4 *>(kn + (4 * i + g) * 16);
+                const u32x4 a = p[0], b = p[1];
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    kw[8 * i + x] = a[x];
+                    kw[8 * i + 4 + x] = b[x];
+                }
             }
         }
-    }
-    if (has_v) {
+        if (g == (tn >> 2)) {
 #pragma unroll
-        for (int c = 0; c < D / 32; c++) vw[c] = (uint32_t)vn[32 * c + j] | (uint32_t)vn[32 * c + 16 + j] << 16;
+            for (int c = 0; c < D / 16; c++) v[c] = vn[16 * c + j];
+        }
     }
+};
+template <int D, class E>
+__device__ __forceinline__ void decode_take_new_token(const AttnArgs &A, const NewToken8<D> &row, int kvh, int id, int tn, int j, int g, int &exponents, DecodePage8<D> &st) {
+    const int64_t pair = (int64_t)id * A.Hkv + kvh;
+    const auto &kw = row.kw;
+    uint32_t vw[D / 32];
+#pragma unroll
+    for (int c = 0; c < D / 32; c++) {
+        uint32_t a = row.v[2 * c], b = row.v[2 * c + 1];
+        asm volatile("" : "+v"(a), "+v"(b));  // paired up here, not where they are requested, which would wait for them
+        vw[c] = a | b << 16;
+    }
+    const bool has_k = j == tn, has_v = g == (tn >> 2);
     Quantiser<E> qk(0, 0, 0), qv(0, 0, 0);
     page_quantisers<E>(kw, vw, exponents, tn > 0, qk, qv);
     exponents = (qk.e + 127) | (qv.e + 127) << 8;
@@ -1373,11 +1392,14 @@ __device__ __forceinline__ void decode_sweep(const AttnArgs &A, int kvh, int qro
         // The last page first (lane 0 holds its id): it alone may be partial, and it is the one that the sequence's new token goes into, which costs no page of
         // the stream behind it its place in the ring.  Every step of the loop fetches, so that the compiler's count of the loads in flight is exact (see below): its last turn
         // may fetch up to NS - 1 pages that no step consumes, a page of the range again, out of L2.
+        const int tn = (n_tok - 1) & (kBlock - 1);
+        NewToken8<D> row;
+        if (takes_new) row.load(A, kvh, qrow, tn, j, g);
 #pragma unroll
         for (int u = 0; u < NS; u++) decode_fetch<D>(A, kvh, __builtin_amdgcn_readlane(my_page, u), j, g, st[u]);
         int exponents = __builtin_amdgcn_readlane(my_scales, 0);
         if (takes_new)
-            decode_take_new_token<D, E>(A, kvh, qrow, __builtin_amdgcn_readlane(my_page, 0), (n_tok - 1) & (kBlock - 1), j, g, exponents, st[0]);
+            decode_take_new_token<D, E>(A, row, kvh, __builtin_amdgcn_readlane(my_page, 0), tn, j, g, exponents, st[0]);
         decode_consume<D, E>(A, st[0], exponents, qreg, n_tok - (n_pg - 1) * kBlock, g, o, m_run, l_run);
         int at = 1;
         for (; at + NS <= n_pg; at += NS) {

@@ -160,7 +160,9 @@ int launch_kv_migrate(const tc_plan *p, bool import, int page0, int n_pages, int
 // A cache in 8 bits (tc_kvq.hip).
 int launch_kvq_append(const tc_plan *p, const tc_kvq_pool *pool, const void *k_new, const void *v_new, void *stream);
 int launch_kvq_read(const tc_plan *p, const tc_kvq_pool *pool, int page0, int n_pages, void *k_out, void *v_out, void *stream);
-// k_new / v_new non-null and no prefill chunk in the batch: the kernel also stores the rows.
+// Whether tc_kvq_mixed_attention_append stores the rows in a launch of its own, before the attention.
+bool kvq_append_apart(const tc_plan *p);
+// k_new / v_new non-null (not where the rows are stored apart): the kernel also stores the rows.
 int launch_kvq_attention(const tc_plan *p, const tc_kvq_pool *pool, const void *q, const void *k_new, const void *v_new, void *out, float scale, void *workspace,
                          void *stream);
 int current_device(int *device);
