@@ -519,15 +519,20 @@ struct TileWidener {
     // undefined bytes: they get probability 0, but V must be finite for the MFMA, so zero.  So must be a token's V for the rows that do not
     // attend over it yet (`diagonal`: the tile has such tokens): a NaN there becomes zero too, which is flagged, and the rows that do attend over it
     // get theirs at the end of the sweep (restore_nan).
-    __device__ __forceinline__ void widen(int stage, int tile_stage, int n_valid, bool diagonal, int lane) const {
+    // `between` runs when the page has been read from its stage: the next fetch into it.
+    __device__ __forceinline__ int exponent(int stage) const { return *reinterpret_cast<const uint8_t *>(slots + (1 + stage) * 256); }
+    template <class F>
+    __device__ __forceinline__ void widen(int stage, int exponent, int tile_stage, int n_valid, bool diagonal, int lane, const F &between) const {
         const char *from = raw + stage * L::kRawPage;
         char *to = dst + tile_stage * C::kTileBytes;
-        const float scale = scale_of(__builtin_amdgcn_readfirstlane((int)*reinterpret_cast<const uint8_t *>(slots + (1 + stage) * 256)));
+        const float scale = scale_of(__builtin_amdgcn_readfirstlane(exponent));
         if (!is_v) {
             // piece = 16 elements (d/16 = c) of one token; in 16 bits two pieces of eight, 2 c and 2 c + 1
             u32x4 w[kRuns];
 #pragma unroll
             for (int i = 0; i < kRuns; i++) w[i] = *reinterpret_cast<const u32x4 *>(from + i * 1024 + lane * 16);
+            reads_done();
+            between();
             char *at = to + (lane >> 4) * (2 * kBlock * 16) + (lane & 15) * 16;
 #pragma unroll
             for (int i = 0; i < kRuns; i++) {
@@ -541,6 +546,8 @@ struct TileWidener {
             const int half = lane >> 5, g = (lane >> 4) & 1, j = lane & 15;
             const char *p = from + (lane + half * 32) * (4 * W);
             piece a = *reinterpret_cast<const piece *>(p), b = *reinterpret_cast<const piece *>(p + 32 * (4 * W));
+            reads_done();
+            between();
             if (n_valid < kBlock) {
                 const uint32_t ma = first_bytes(n_valid - 4 * g), mb = first_bytes(n_valid - 4 * g - 8);
 #pragma unroll
@@ -566,9 +573,8 @@ struct TileWidener {
 #pragma unroll
             for (int c = 0; c < W; c++) *reinterpret_cast<typename E::x8 *>(at + c * 1024) = E::widen8(a[c], b[c], scale);
         }
-        // the next fetch into this stage comes after these reads
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
+    static __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 };
 
 // Rare: the sweep of a prefill item, over tokens up to `end`, met NaN among the V of tokens from `first` on, which not all rows attend over, and put
@@ -800,11 +806,10 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         wd.fetch(ids[C::kTilePages], 1);
         page_id_fetch(pages + page_index(t_begin + 4), wd.id_slot());
         wait_loads_but<TileWidener<D, E>::kLoads + 1>();
-        wd.widen(0, 0, kv_len - (t_begin * C::kTilePages + pg) * kBlock, diagonal(t_begin), lane);
-        wd.fetch(ids[2 * C::kTilePages], 0);
+        wd.widen(0, wd.exponent(0), 0, kv_len - (t_begin * C::kTilePages + pg) * kBlock, diagonal(t_begin), lane, [&] { wd.fetch(ids[2 * C::kTilePages], 0); });
         wait_loads_but<TileWidener<D, E>::kLoads + 1>();
-        if (n_sweep > 1) wd.widen(1, 1, kv_len - ((t_begin + 1) * C::kTilePages + pg) * kBlock, diagonal(t_begin + 1), lane);
-        wd.fetch(ids[3 * C::kTilePages], 1);
+        wd.widen(1, wd.exponent(1), 1, kv_len - ((t_begin + 1) * C::kTilePages + pg) * kBlock, n_sweep > 1 && diagonal(t_begin + 1), lane,
+                 [&] { wd.fetch(ids[3 * C::kTilePages], 1); });
     } else if (copier) {
         // In the order in which the sweep needs them.  The ids of all these pages lie in the record, so that only two accesses to
         // memory follow one after the other before the first product: the record, and the tiles (and Q).
@@ -916,12 +921,21 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
     // One step for tile t_begin + j, which lives in stages s0 = j mod NS and v0 = j mod VS: `sc` holds the scores of its
     // first half, `kf` the K fragments of its second half.  NEXT: tile j + 1 exists.
     int s0 = 0, v0 = 0;
+    // A cache in 8 bits: the page id of the next fetch, and the exponent of the page widened next, which is in raw stage `stage`.
+    [[maybe_unused]] auto next_of_widener = [&](int stage) {
+        if constexpr (KVQ) {
+            const int id = *reinterpret_cast<const int *>(wd.id_slot() + 4 * lane), e = wd.exponent(stage);
+            id_next[0] = __builtin_amdgcn_readfirstlane(id);
+            id_next[1] = __builtin_amdgcn_readfirstlane(e);
+        }
+    };
     auto copies = [&](int j) {  // K(j+NS) replaces K(j), V(j+VS-1) replaces V(j-1)
         const int vm1 = v0 == 0 ? VS - 1 : v0 - 1;
-        if constexpr (KVQ) {  // tile j + 2 replaces tile j - 1
-            if (j + 2 < n_sweep) wd.widen(j & 1, vm1, kv_len - ((t_begin + j + 2) * C::kTilePages + pg) * kBlock, diagonal(t_begin + j + 2), lane);
-            page_id_fetch(pages + page_index(t_begin + j + 5), wd.id_slot());
-            wd.fetch(id_next[0], j & 1);
+        if constexpr (KVQ) {  // tile j + 2 replaces tile j - 1 (past the end of the range the tile is never read)
+            wd.widen(j & 1, id_next[1], vm1, kv_len - ((t_begin + j + 2) * C::kTilePages + pg) * kBlock, j + 2 < n_sweep && diagonal(t_begin + j + 2), lane, [&] {
+                page_id_fetch(pages + page_index(t_begin + j + 5), wd.id_slot());
+                wd.fetch(id_next[0], j & 1);
+            });
         } else if constexpr (NW == kMixedWaves) {
             // First the page ids for the next step's copies.  They are counted by vmcnt like the copies.
             page_id_fetch(pages + page_index(t_begin + j + 1 + NS), idk_slot);
@@ -937,7 +951,7 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         if constexpr (KVQ) wait_loads_but<TileWidener<D, E>::kLoads>();
         else wait_loads_but<VS == 3 ? 2 * C::kRuns : C::kRuns>();
         if constexpr (KVQ) {
-            id_next[0] = page_id_read(wd.id_slot(), lane);
+            next_of_widener((j + 1) & 1);
         } else if constexpr (NW == kMixedWaves) {
             id_next[2] = page_id_read(idk_slot, lane);
             id_next[VS - 2] = page_id_read(idv_slot, lane);
@@ -963,9 +977,11 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         // every wave is done with step j - 1; the copies waited for at its end (a cache in 8 bits: the tile widened in it) are visible
         if constexpr (KVQ) barrier_lds();
         else __syncthreads();
-        if (NEXT && copier) copies(j);  // past the end of the range the copies are never read
+        // (A cache in 8 bits: waves 0-3 widen before the first phase, waves 4-7 before the second, so that a SIMD's other wave has products under way.)
+        if (NEXT && copier && !(KVQ && wave >= C::kTilePages)) copies(j);  // past the end of the range the copies are never read
         const std::true_type yes;
         phase(v_cur, 0, k_nxt, 0, sc, sn, tile * C::kTileTokens + 32, mask_tag, yes, next_tag);
+        if (KVQ && NEXT && wave >= C::kTilePages) copies(j);
         phase(v_cur, 1, k_nxt, 1, sn, sc, (tile + 1) * C::kTileTokens, mask_tag, next_tag, next_tag);
         if (NEXT && copier) {
             copies_landed(j);
@@ -981,7 +997,7 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         // other loop wait for all copies in flight, and 17 tokens at 6966 beside 6 decodes take 53 us a layer instead of 47.)
         if constexpr (KVQ) {
             wait_loads_but<TileWidener<D, E>::kLoads>();
-            id_next[0] = page_id_read(wd.id_slot(), lane);
+            next_of_widener(0);
         } else if (copier) wait_loads_but<(NS + VS - 4) * C::kRuns>();
         for (int j = 0; j < n_sweep; j++) {
             if constexpr (KVQ) barrier_lds();
@@ -1014,7 +1030,7 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         const int n_plain = max(0, min(n_sweep - 1, (wave_pmin + 1) / C::kTileTokens - t_begin - 1));
         if constexpr (KVQ) {  // tile 2, for step 0, and the page id of its fetch
             wait_loads_but<TileWidener<D, E>::kLoads>();
-            id_next[0] = page_id_read(wd.id_slot(), lane);
+            next_of_widener(0);
         } else if (copier) wait_loads_but<(NS + VS - 4) * C::kRuns>();  // K(1), for step 0; the others are waited for in its end
         int j = 0;
         for (; j < n_plain; j++) step(j, no, yes);
@@ -1087,7 +1103,11 @@ struct DecodePage8 {
     piece v[2];
 };
 template <int D, class E> using DecodePageOf = std::conditional_t<E::kKvq, DecodePage8<D>, DecodePage<D>>;
-constexpr int kDecodeStages8 = 4, kWideStages8 = 6;
+// Pages of a cache in 8 bits in registers per wave, half the size.  Measured over 21 batches, 2 / 3 / 4 / 5 of them in single waves and 8 / 4 / 6 / 5 in
+// whole workgroups of decodes only: 3.4 / 0 / 1.7 / 2.2 % slower (few decodes lose by more, whose waves wait for the first of them), 3 in whole workgroups 0.6 %
+// faster than 4 at head_dim 128, up to 3 % slower at 64.
+constexpr int kDecodeStages8 = 3;
+constexpr int wide_stages8(int head_dim) { return head_dim == 128 ? 3 : 4; }
 
 // KV pages are read exactly once per launch, by one wavefront: stream them past the caches.
 // When the attention kernel also does the append (a batch of decodes: tc_mixed_attention_append), the newest
@@ -1131,46 +1151,36 @@ __device__ __forceinline__ void decode_take_new_token(const AttnArgs &A, int kvh
 // while this one reads the page, so the wavefront always does.  It quantises the row as kvq_append_kernel does and stores what has changed: the
 // row's 16-byte pieces of K, the 16-byte pieces of V that hold its bytes, all older rows where a scale grows (rare), and the exponents.
 // The row is requested before the pages of the ring: loads complete in order, and behind them it would have the wave wait for all of those.
+// (All lanes request it, and those that hold no part of it drop what they get: a branch here has the compiler wait for it at once.)
 template <int D>
 struct NewToken8 {
-    uint32_t kw[D / 8], v[D / 16];  // 16 elements d = 16 (4 i + g) .. for each piece of K; d = 16 c + j for each byte of V
-    __device__ __forceinline__ void load(const AttnArgs &A, int kvh, int qrow, int tn, int j, int g) {
+    u32x4 k[D / 64][2];   // 16 elements d = 16 (4 i + g) .. for each piece of K
+    uint32_t v[D / 16];   // d = 16 c + j for each byte of V
+    __device__ __forceinline__ void load(const AttnArgs &A, int kvh, int qrow, int j, int g) {
         const int64_t src = ((int64_t)qrow * A.Hkv + kvh) * D;
-        const uint16_t *kn = A.k_new + src, *vn = A.v_new + src;
+        const u32x4 *kn = reinterpret_cast<const u32x4 *>(A.k_new + src);
 #pragma unroll
-        for (int i = 0; i < D / 8; i++) kw[i] = 0;
-#pragma unroll
-        for (int i = 0; i < D / 16; i++) v[i] = 0;
-        if (j == tn) {
-#pragma unroll
-            for (int i = 0; i < D / 64; i++) {
-                const u32x4 *p = reinterpret_cast<const u32x4 *>(kn + (4 * i + g) * 16);
-                const u32x4 a = p[0], b = p[1];
-#pragma unroll
-                for (int x = 0; x < 4; x++) {
-                    kw[8 * i + x] = a[x];
-                    kw[8 * i + 4 + x] = b[x];
-                }
-            }
+        for (int i = 0; i < D / 64; i++) {
+            k[i][0] = kn[2 * (4 * i + g)];
+            k[i][1] = kn[2 * (4 * i + g) + 1];
         }
-        if (g == (tn >> 2)) {
 #pragma unroll
-            for (int c = 0; c < D / 16; c++) v[c] = vn[16 * c + j];
-        }
+        for (int c = 0; c < D / 16; c++) v[c] = A.v_new[src + 16 * c + j];
     }
 };
 template <int D, class E>
 __device__ __forceinline__ void decode_take_new_token(const AttnArgs &A, const NewToken8<D> &row, int kvh, int id, int tn, int j, int g, int &exponents, DecodePage8<D> &st) {
     const int64_t pair = (int64_t)id * A.Hkv + kvh;
-    const auto &kw = row.kw;
-    uint32_t vw[D / 32];
+    const bool has_k = j == tn, has_v = g == (tn >> 2);
+    uint32_t kw[D / 8], vw[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 8; i++) kw[i] = has_k ? row.k[i / 8][(i / 4) & 1][i & 3] : 0u;
 #pragma unroll
     for (int c = 0; c < D / 32; c++) {
         uint32_t a = row.v[2 * c], b = row.v[2 * c + 1];
         asm volatile("" : "+v"(a), "+v"(b));  // paired up here, not where they are requested, which would wait for them
-        vw[c] = a | b << 16;
+        vw[c] = has_v ? a | b << 16 : 0u;
     }
-    const bool has_k = j == tn, has_v = g == (tn >> 2);
     Quantiser<E> qk(0, 0, 0), qv(0, 0, 0);
     page_quantisers<E>(kw, vw, exponents, tn > 0, qk, qv);
     exponents = (qk.e + 127) | (qv.e + 127) << 8;
@@ -1394,7 +1404,7 @@ __device__ __forceinline__ void decode_sweep(const AttnArgs &A, int kvh, int qro
         // may fetch up to NS - 1 pages that no step consumes, a page of the range again, out of L2.
         const int tn = (n_tok - 1) & (kBlock - 1);
         NewToken8<D> row;
-        if (takes_new) row.load(A, kvh, qrow, tn, j, g);
+        if (takes_new) row.load(A, kvh, qrow, j, g);
 #pragma unroll
         for (int u = 0; u < NS; u++) decode_fetch<D>(A, kvh, __builtin_amdgcn_readlane(my_page, u), j, g, st[u]);
         int exponents = __builtin_amdgcn_readlane(my_scales, 0);
@@ -1641,7 +1651,7 @@ __device__ __forceinline__ void decode_item_wide(const AttnArgs &A, const int32_
     stores_done();
     const int32_t *mg = A.merge + (int64_t)merge_item * kItemInts;
     if (!workgroup_arrives_last(A.counters + mg[MG_COUNTER], mg[MG_NSPLIT], reinterpret_cast<int *>(lds), tid)) return;
-    merge_pair<D, E, true, STORE && D == 128 ? kWideMergeBatch : kMergeBatch>(A.ws_o, A.ws_ml, mg[MG_SLOT0], mg[MG_NSPLIT], G,
+    merge_pair<D, E, true, STORE && D == 128 && !E::kKvq ? kWideMergeBatch : kMergeBatch>(A.ws_o, A.ws_ml, mg[MG_SLOT0], mg[MG_NSPLIT], G,
                                                                              A.out + ((int64_t)qrow * A.Hq + kvh * G) * D, lds, tid, R * 64);
 }
 
@@ -1811,8 +1821,10 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == kMixedWaves ? 1 : CHUNK ?
 // A batch of few decodes: one workgroup of kWideWaves waves per split, or per two (decode_item_wide), one or two per compute unit, with
 // registers for kWideStages - 1 pages in flight per wave; the wave that takes a sequence's new token from k_new / v_new also
 // stores its row.  Arguments as above; the prefill lists are empty.
+// A cache in 8 bits leaves registers for three workgroups to a unit, with eight partial results requested at once (200 decodes of 150-450 tokens, 32/8 heads,
+// head_dim 128, 25.8 -> 24.1 us, 12 of 3000-9000 27.0 -> 26.5, 13 other batches 0.2 % faster on the mean).
 template <int D, class E, int W>
-__global__ void __launch_bounds__(kWideWaves * 64, 2)
+__global__ void __launch_bounds__(kWideWaves * 64, E::kKvq ? 3 : 2)
     wide_decode_kernel(uint16_t *k_pool, uint16_t *v_pool, const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_new,
                        const uint16_t *__restrict__ v_new, uint16_t *__restrict__ out, const int32_t *__restrict__ pages,
                        const int32_t *__restrict__ decode, const int32_t *__restrict__ merge, int32_t *counters, float *ws,
@@ -1827,7 +1839,7 @@ __global__ void __launch_bounds__(kWideWaves * 64, 2)
     A.ws_o = ws; A.ws_ml = ws + (int64_t)sc.n_partials * sc.G * D;
     A.n_decode = sc.n_decode; A.Hq = sc.Hq; A.Hkv = sc.Hkv; A.G = sc.G; A.fused = sc.fused; A.scale_log2 = sc.scale_log2;
     A.scales = sc.scales;
-    decode_item_wide<D, E, E::kKvq ? kWideStages8 : kWideStages, kWideWaves, W, true>(A, decode + (int64_t)blockIdx.x * W * kItemInts, reinterpret_cast<float *>(lds));
+    decode_item_wide<D, E, E::kKvq ? wide_stages8(D) : kWideStages, kWideWaves, W, true>(A, decode + (int64_t)blockIdx.x * W * kItemInts, reinterpret_cast<float *>(lds));
 #ifdef TC_WG_TRACE
     wg_trace(t_start, t_start, true);
 #endif
