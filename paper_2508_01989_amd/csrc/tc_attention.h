@@ -477,8 +477,9 @@ __device__ __forceinline__ void barrier_lds() {
 }
 
 // A cache in 8 bits: wave w of the eight moves page w mod 4 of every tile, K (w < 4) or V^T, in two steps.  fetch() copies the page as it
-// lies in the pool into a stage of the wave's own, with direct-to-LDS loads, and beside it the exponent of its scale;
-// widen() reads it back a step or more later and leaves it in the tile's stage in 16 bits, in the layout that the sweep reads.  A byte is
+// lies in the pool into a stage of the wave's own, with direct-to-LDS loads, and beside it the exponent of its scale.
+// A step or more later read() takes it back, 32 bytes a lane at head_dim 128 (16 at 64), and store_piece() leaves it in the tile's stage in 16 bits, in the layout that the
+// sweep reads: eight elements at a time, so that the sweep can put a piece under each of its first products.  A byte is
 // thus widened once per workgroup, two per instruction, and 16 KiB of a tile cross LDS once more; widened by every wave behind its
 // operand reads it would be eight times.
 template <int D, class E>
@@ -486,13 +487,16 @@ struct TileWidener {
     using C = PrefillCfg<D>;
     using L = PrefillLds<D, kMixedWaves, true>;
     static constexpr int kRuns = L::kRawPage / 1024;
-    static constexpr int kLoads = kRuns + 1;  // of a fetch
+    static constexpr int kLoads = kRuns + 1;   // of a fetch
+    static constexpr int kPieces = 2 * kRuns;  // of a lane: eight elements each
     typedef const __attribute__((address_space(1))) void *gptr_t;
     typedef __attribute__((address_space(3))) void *lptr_t;
     const uint8_t *src, *scales;  // pool + this lane's offset inside a (page, KV head) block; this head's exponent of block 0
+    int second;                   // what is fetched into the second KiB of a stage lies so far behind what goes into the first
     char *raw, *slots;            // this wave's stages and slots
     int *flag;                    // this wave's
-    char *dst;                    // this wave's page in stage 0 of its tensor
+    char *dst;                    // where this lane's first piece goes in stage 0 of the wave's tensor and page
+    int odd;                      // and how far behind an even piece the odd one goes
     int64_t page_stride;          // bytes per page (all KV heads)
     int scale_stride;
     bool is_v;
@@ -502,76 +506,85 @@ struct TileWidener {
         page_in_tile = wave & (C::kTilePages - 1);
         page_stride = (int64_t)A.Hkv * L::kRawPage;
         scale_stride = A.Hkv * 2;
-        src = reinterpret_cast<const uint8_t *>(is_v ? A.v_pool : A.k_pool) + (int64_t)kvh * L::kRawPage + lane * 16;
+        // K: the lane widens d = 16 (lane / 16) .. + 15 of token lane % 16, and 64 further on.  In 16 bits pieces 2 and 3 lie 2 KiB behind 0 and 1.
+        // V: tokens 4 g .. 4 g + 3 and 4 (g + 2) .. of d = 16 half + j + 32 c, half a row of 16 slots for each c: pieces lie 1 KiB apart.  Eight lanes
+        // store four whole rows, 128 bytes of LDS, which is what it takes in at once; at head_dim 128 the pool's 16-byte pieces are fetched in the order of the lanes
+        // that widen them, so that these read them back in line.
+        const int half = lane >> 5, g = lane & 1, j = (lane >> 1) & 15;
+        src = reinterpret_cast<const uint8_t *>(is_v ? A.v_pool : A.k_pool) + (int64_t)kvh * L::kRawPage + (is_v && D == 128 ? half * 64 + g * 16 + j : lane) * 16;
+        second = is_v ? 512 : 1024;
         scales = A.scales + kvh * 2 + (is_v ? 1 : 0);
         raw = lds + L::kRaw + wave * (L::kRawStages * L::kRawPage);
         slots = lds + L::kIds + wave * (L::kSlots * 256);
         flag = reinterpret_cast<int *>(lds + L::kFlags) + wave;
-        dst = lds + (is_v ? L::kV : 0) + page_in_tile * C::kPageBytes;
+        dst = lds + (is_v ? L::kV : 0) + page_in_tile * C::kPageBytes +
+              (is_v ? (16 * half + j) * 32 + (g ^ (j >> 3)) * 16 : (lane >> 4) * (2 * kBlock * 16) + (lane & 15) * 16);
+        odd = is_v ? 1024 : kBlock * 16;
     }
     __device__ __forceinline__ char *id_slot() const { return slots; }
     __device__ __forceinline__ void fetch(int page_id, int stage) const {
         const int64_t id = __builtin_amdgcn_readfirstlane(page_id);
-        lds_load_runs<kRuns>((gptr_t)(src + id * page_stride), (lptr_t)(raw + stage * L::kRawPage));
+        const uint8_t *from = src + id * page_stride;
+        char *to = raw + stage * L::kRawPage;
+        __builtin_amdgcn_global_load_lds((gptr_t)from, (lptr_t)to, 16, 0, 0);
+        if constexpr (kRuns > 1) __builtin_amdgcn_global_load_lds((gptr_t)(from + second - 1024), (lptr_t)to, 16, 1024, 0);  // (the offset counts on both sides)
         __builtin_amdgcn_global_load_lds((gptr_t)(scales + id * scale_stride), (lptr_t)(slots + (1 + stage) * 256), 1, 0, 0);
     }
-    // The page in `stage`, whose loads have landed, into the 16-bit stage `tile_stage`; its first n_valid tokens are real.  Slots behind those hold
-    // undefined bytes: they get probability 0, but V must be finite for the MFMA, so zero.  So must be a token's V for the rows that do not
-    // attend over it yet (`diagonal`: the tile has such tokens): a NaN there becomes zero too, which is flagged, and the rows that do attend over it
-    // get theirs at the end of the sweep (restore_nan).
-    // `between` runs when the page has been read from its stage: the next fetch into it.
-    __device__ __forceinline__ int exponent(int stage) const { return *reinterpret_cast<const uint8_t *>(slots + (1 + stage) * 256); }
-    template <class F>
-    __device__ __forceinline__ void widen(int stage, int exponent, int tile_stage, int n_valid, bool diagonal, int lane, const F &between) const {
+    // The exponent in its lowest byte, in every lane.
+    __device__ __forceinline__ int exponent(int stage) const { return *reinterpret_cast<const int *>(slots + (1 + stage) * 256); }
+    static __device__ __forceinline__ float scale(int exponent) { return scale_of(__builtin_amdgcn_readfirstlane(exponent) & 0xFF); }
+    // This lane's words of the page in `stage`, whose loads have landed, the same way for either tensor, so that nothing has to be moved (which
+    // would wait for them).  Piece i is words 2 i and 2 i + 1 of K, i and kPieces + i of V.
+    __device__ __forceinline__ void read(int stage, int lane, uint32_t (&w)[2 * kPieces]) const {
         const char *from = raw + stage * L::kRawPage;
-        char *to = dst + tile_stage * C::kTileBytes;
-        const float scale = scale_of(__builtin_amdgcn_readfirstlane(exponent));
-        if (!is_v) {
-            // piece = 16 elements (d/16 = c) of one token; in 16 bits two pieces of eight, 2 c and 2 c + 1
-            u32x4 w[kRuns];
+        typedef uint32_t part __attribute__((ext_vector_type(kPieces)));
+        const int at = D == 128 ? lane * 16 : is_v ? ((lane >> 5) * 64 + (lane & 1) * 16 + ((lane >> 1) & 15)) * 8 : lane * 16;
+        const part a = *reinterpret_cast<const part *>(from + at), b = *reinterpret_cast<const part *>(from + at + (D == 128 ? 1024 : is_v ? 256 : 8));
 #pragma unroll
-            for (int i = 0; i < kRuns; i++) w[i] = *reinterpret_cast<const u32x4 *>(from + i * 1024 + lane * 16);
-            reads_done();
-            between();
-            char *at = to + (lane >> 4) * (2 * kBlock * 16) + (lane & 15) * 16;
+        for (int i = 0; i < kPieces; i++) {
+            w[i] = a[i];
+            w[kPieces + i] = b[i];
+        }
+    }
+    // Only the first n_valid tokens of a page of V are real: slots behind those hold undefined bytes, which get probability 0 but must be finite for the
+    // MFMA, so zero.  So must be a token's V for the rows that do not attend over it yet (`diagonal`: the tile has such tokens): a NaN there becomes
+    // zero too, which is flagged, and the rows that do attend over it get theirs at the end of the sweep (restore_nan).
+    __device__ __forceinline__ void clean(uint32_t (&w)[2 * kPieces], int n_valid, bool diagonal, int lane) const {
+        if (!is_v) return;
+        if (n_valid < kBlock) {
+            const int g = lane & 1;
+            const uint32_t ma = first_bytes(n_valid - 4 * g), mb = first_bytes(n_valid - 4 * g - 8);
 #pragma unroll
-            for (int i = 0; i < kRuns; i++) {
-                *reinterpret_cast<typename E::x8 *>(at + i * (8 * kBlock * 16)) = E::widen8(w[i][0], w[i][1], scale);
-                *reinterpret_cast<typename E::x8 *>(at + i * (8 * kBlock * 16) + kBlock * 16) = E::widen8(w[i][2], w[i][3], scale);
+            for (int i = 0; i < kPieces; i++) {
+                w[i] &= ma;
+                w[kPieces + i] &= mb;
             }
-        } else {
-            // piece (half, g, j) = tokens 4 g .. 4 g + 3 of d = 32 c + 16 half + j, c < D/32; pieces g and g + 2 make half a row of 16 slots for each c
-            constexpr int W = D / 32;
-            typedef uint32_t piece __attribute__((ext_vector_type(W)));
-            const int half = lane >> 5, g = (lane >> 4) & 1, j = lane & 15;
-            const char *p = from + (lane + half * 32) * (4 * W);
-            piece a = *reinterpret_cast<const piece *>(p), b = *reinterpret_cast<const piece *>(p + 32 * (4 * W));
-            reads_done();
-            between();
-            if (n_valid < kBlock) {
-                const uint32_t ma = first_bytes(n_valid - 4 * g), mb = first_bytes(n_valid - 4 * g - 8);
+        }
+        if (diagonal) {
+            uint32_t any = 0;
 #pragma unroll
-                for (int c = 0; c < W; c++) {
-                    a[c] &= ma;
-                    b[c] &= mb;
-                }
+            for (int i = 0; i < 2 * kPieces; i++) any |= nan_bytes(w[i]);
+            if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
+#pragma unroll
+                for (int i = 0; i < 2 * kPieces; i++) w[i] &= ~((nan_bytes(w[i]) >> 7) * 255u);
+                *flag = 1;
             }
-            if (diagonal) {
-                uint32_t any = 0;
-#pragma unroll
-                for (int c = 0; c < W; c++) any |= nan_bytes(a[c]) | nan_bytes(b[c]);
-                if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
-#pragma unroll
-                    for (int c = 0; c < W; c++) {
-                        a[c] &= ~((nan_bytes(a[c]) >> 7) * 255u);
-                        b[c] &= ~((nan_bytes(b[c]) >> 7) * 255u);
-                    }
-                    *flag = 1;
-                }
-            }
-            char *at = to + (16 * half + j) * 32 + (g ^ (j >> 3)) * 16;
-#pragma unroll
-            for (int c = 0; c < W; c++) *reinterpret_cast<typename E::x8 *>(at + c * 1024) = E::widen8(a[c], b[c], scale);
+        }
+    }
+    __device__ __forceinline__ char *even_piece(int tile_stage) const { return dst + tile_stage * C::kTileBytes; }
+    template <int I>
+    __device__ __forceinline__ void store_piece(const uint32_t (&w)[2 * kPieces], float scale, char *even, char *odd) const {
+        const uint32_t lo = is_v ? w[I] : w[2 * I], hi = is_v ? w[kPieces + I] : w[2 * I + 1];
+        *reinterpret_cast<typename E::x8 *>((I & 1 ? odd : even) + (I >> 1) * 2048) = E::widen8(lo, hi, scale);
+    }
+    __device__ __forceinline__ void store(const uint32_t (&w)[2 * kPieces], int exponent, int tile_stage) const {
+        const float s = scale(exponent);
+        char *const at = even_piece(tile_stage);
+        store_piece<0>(w, s, at, at + odd);
+        store_piece<1>(w, s, at, at + odd);
+        if constexpr (kPieces > 2) {
+            store_piece<2>(w, s, at, at + odd);
+            store_piece<3>(w, s, at, at + odd);
         }
     }
     static __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
@@ -689,6 +702,11 @@ struct PrefillWave {
     }
 };
 
+template <class F, int... I>
+__device__ __forceinline__ void for_each_index(const F &f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
+template <int N, class F>
+__device__ __forceinline__ void for_each_index(const F &f) { for_each_index(f, std::make_integer_sequence<int, N>()); }
+
 // The reference maximum of a row (log2 domain) is kept while it serves: probabilities may exceed 1 as long
 // as fp32 sums and 16-bit operands hold them without loss of relative precision, so O has to be rescaled
 // only a few times per sweep instead of whenever any of a wave's 32 rows sees a new maximum, and the row
@@ -799,6 +817,9 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
     int window = 0;
     char *const idk_slot = lds + L::kIds + (2 * wave) * kIdSlotBytes, *const idv_slot = idk_slot + kIdSlotBytes;
     auto page_index = [&](int tile) { return min(tile * C::kTilePages + pg, n_pages - 1); };  // past the end: the last page, whose copy is never used
+    // The page that this wave widens in the next step, as it lies in the pool, and the exponent of its scale.
+    [[maybe_unused]] uint32_t raw[KVQ ? D / 16 : 1];
+    [[maybe_unused]] int raw_exponent = 0;
     if constexpr (KVQ) {
         const int32_t *ids = rec + RC_IDS + pg;
         *wd.flag = 0;
@@ -806,10 +827,19 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         wd.fetch(ids[C::kTilePages], 1);
         page_id_fetch(pages + page_index(t_begin + 4), wd.id_slot());
         wait_loads_but<TileWidener<D, E>::kLoads + 1>();
-        wd.widen(0, wd.exponent(0), 0, kv_len - (t_begin * C::kTilePages + pg) * kBlock, diagonal(t_begin), lane, [&] { wd.fetch(ids[2 * C::kTilePages], 0); });
+        wd.read(0, lane, raw);
+        int e = wd.exponent(0);
+        wd.reads_done();
+        wd.fetch(ids[2 * C::kTilePages], 0);
+        wd.clean(raw, kv_len - (t_begin * C::kTilePages + pg) * kBlock, diagonal(t_begin), lane);
+        wd.store(raw, e, 0);
         wait_loads_but<TileWidener<D, E>::kLoads + 1>();
-        wd.widen(1, wd.exponent(1), 1, kv_len - ((t_begin + 1) * C::kTilePages + pg) * kBlock, n_sweep > 1 && diagonal(t_begin + 1), lane,
-                 [&] { wd.fetch(ids[3 * C::kTilePages], 1); });
+        wd.read(1, lane, raw);
+        e = wd.exponent(1);
+        wd.reads_done();
+        wd.fetch(ids[3 * C::kTilePages], 1);
+        wd.clean(raw, kv_len - ((t_begin + 1) * C::kTilePages + pg) * kBlock, n_sweep > 1 && diagonal(t_begin + 1), lane);
+        wd.store(raw, e, 1);
     } else if (copier) {
         // In the order in which the sweep needs them.  The ids of all these pages lie in the record, so that only two accesses to
         // memory follow one after the other before the first product: the record, and the tiles (and Q).
@@ -918,24 +948,72 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         }
         settle(cur);
     };
+    // The same for a cache in 8 bits, with both tiles to prepare: `piece`(i) is work that goes under product i, for the first of them, whose VALU slots are free.  The order is
+    // that of the source, a region to each product: asked of the compiler as above it had the second product's eight MFMAs in a row, and a sweep took 17 % longer.
+    [[maybe_unused]] auto ordered_phase = [&](lds_cptr v_h, int hv, lds_cptr k_after, int hk, f32x16 &cur, f32x16 &nxt, int tok_nxt, auto mask_tag, const auto &piece) {
+        constexpr int kFirst = D == 128 ? 5 : 0;  // the first product with softmax work under it: two elements for each of eight
+        x8 pn[2];
+        psum = 0.f;
+        // (sums and roundings a product later than the exponentials they wait for)
+        float p[2];
+        const auto softmax = [&](auto g) {
+            constexpr int i = (decltype(g)::value - kFirst) * 2;
+            if constexpr (i >= 2 && i <= 16) {
+                psum += p[0];
+                psum += p[1];
+                pn[(i - 2) >> 3][(i - 2) & 7] = (el)p[0];
+                pn[(i - 2) >> 3][(i - 1) & 7] = (el)p[1];
+            }
+            if constexpr (i >= 0 && i < 16) {
+                p[0] = fast_exp2(__builtin_fmaf(cur[i], c_log2, -m_run));
+                p[1] = fast_exp2(__builtin_fmaf(cur[i + 1], c_log2, -m_run));
+            }
+        };
+        const auto product = [&](auto g_) {
+            constexpr int g = decltype(g_)::value;
+            if constexpr (g == 0) {
+#pragma unroll
+                for (int r = 0; r < 16; r++) nxt[r] = 0.f;
+            }
+            if constexpr (g < KS) {
+                nxt = E::mfma32(kf[g], qreg[g], nxt);
+                kf[g] = *(typename W::lds_x8ptr)(k_after + 2 * hk * C::kPageBytes + 2 * g * (kBlock * 16));
+            } else {
+                constexpr int b = (g - KS) / MT, c = (g - KS) % MT;
+                o[c] = E::mfma32(vf[b][c], pb[b], o[c]);
+                vf[b][c] = *(typename W::lds_x8ptr)(v_h + (2 * hv + b) * C::kPageBytes + c * (32 * 32));
+            }
+            piece(g_);
+            softmax(g_);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        __builtin_amdgcn_sched_barrier(0);
+        for_each_index<KS + 2 * MT>(product);
+        softmax(std::integral_constant<int, (KS + 2 * MT > kFirst + 8 ? 1000 : kFirst + 8)>());
+        pb[0] = pn[0];
+        pb[1] = pn[1];
+        asm volatile("" : "+v"(pb[0]), "+v"(pb[1]), "+v"(psum));  // computed in this phase: the next one uses them
+        if constexpr (decltype(mask_tag)::value) W::causal_mask(nxt, tok_nxt, hh, p_abs);
+        settle(cur);
+    };
     // One step for tile t_begin + j, which lives in stages s0 = j mod NS and v0 = j mod VS: `sc` holds the scores of its
     // first half, `kf` the K fragments of its second half.  NEXT: tile j + 1 exists.
     int s0 = 0, v0 = 0;
-    // A cache in 8 bits: the page id of the next fetch, and the exponent of the page widened next, which is in raw stage `stage`.
-    [[maybe_unused]] auto next_of_widener = [&](int stage) {
+    // A cache in 8 bits: what the step after needs of LDS, requested before its barrier: the page in raw stage `stage`, its exponent, the page id of the next fetch.
+    [[maybe_unused]] auto read_raw = [&](int stage) {
         if constexpr (KVQ) {
-            const int id = *reinterpret_cast<const int *>(wd.id_slot() + 4 * lane), e = wd.exponent(stage);
-            id_next[0] = __builtin_amdgcn_readfirstlane(id);
-            id_next[1] = __builtin_amdgcn_readfirstlane(e);
+            id_next[0] = *reinterpret_cast<const int *>(wd.id_slot() + 4 * lane);
+            raw_exponent = wd.exponent(stage);
+            wd.read(stage, lane, raw);
         }
     };
+    [[maybe_unused]] auto tokens_of_raw = [&](int j) { return kv_len - ((t_begin + j + 2) * C::kTilePages + pg) * kBlock; };  // real ones, of the page widened in step j
     auto copies = [&](int j) {  // K(j+NS) replaces K(j), V(j+VS-1) replaces V(j-1)
         const int vm1 = v0 == 0 ? VS - 1 : v0 - 1;
         if constexpr (KVQ) {  // tile j + 2 replaces tile j - 1 (past the end of the range the tile is never read)
-            wd.widen(j & 1, id_next[1], vm1, kv_len - ((t_begin + j + 2) * C::kTilePages + pg) * kBlock, j + 2 < n_sweep && diagonal(t_begin + j + 2), lane, [&] {
-                page_id_fetch(pages + page_index(t_begin + j + 5), wd.id_slot());
-                wd.fetch(id_next[0], j & 1);
-            });
+            page_id_fetch(pages + page_index(t_begin + j + 5), wd.id_slot());
+            wd.fetch(id_next[0], j & 1);
+            wd.clean(raw, tokens_of_raw(j), j + 2 < n_sweep && diagonal(t_begin + j + 2), lane);
         } else if constexpr (NW == kMixedWaves) {
             // First the page ids for the next step's copies.  They are counted by vmcnt like the copies.
             page_id_fetch(pages + page_index(t_begin + j + 1 + NS), idk_slot);
@@ -951,7 +1029,7 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         if constexpr (KVQ) wait_loads_but<TileWidener<D, E>::kLoads>();
         else wait_loads_but<VS == 3 ? 2 * C::kRuns : C::kRuns>();
         if constexpr (KVQ) {
-            next_of_widener((j + 1) & 1);
+            read_raw((j + 1) & 1);
         } else if constexpr (NW == kMixedWaves) {
             id_next[2] = page_id_read(idk_slot, lane);
             id_next[VS - 2] = page_id_read(idv_slot, lane);
@@ -977,12 +1055,22 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         // every wave is done with step j - 1; the copies waited for at its end (a cache in 8 bits: the tile widened in it) are visible
         if constexpr (KVQ) barrier_lds();
         else __syncthreads();
-        // (A cache in 8 bits: waves 0-3 widen before the first phase, waves 4-7 before the second, so that a SIMD's other wave has products under way.)
-        if (NEXT && copier && !(KVQ && wave >= C::kTilePages)) copies(j);  // past the end of the range the copies are never read
+        if (NEXT && copier) copies(j);  // past the end of the range the copies are never read
         const std::true_type yes;
-        phase(v_cur, 0, k_nxt, 0, sc, sn, tile * C::kTileTokens + 32, mask_tag, yes, next_tag);
-        if (KVQ && NEXT && wave >= C::kTilePages) copies(j);
-        phase(v_cur, 1, k_nxt, 1, sn, sc, (tile + 1) * C::kTileTokens, mask_tag, next_tag, next_tag);
+        const auto phases = [&] {
+            phase(v_cur, 0, k_nxt, 0, sc, sn, tile * C::kTileTokens + 32, mask_tag, yes, next_tag);
+            phase(v_cur, 1, k_nxt, 1, sn, sc, (tile + 1) * C::kTileTokens, mask_tag, next_tag, next_tag);
+        };
+        if constexpr (!KVQ) phases();
+        else if constexpr (!NEXT) phases();
+        else {
+            const float scale = wd.scale(raw_exponent);
+            char *const even = wd.even_piece(v0 == 0 ? VS - 1 : v0 - 1), *const odd = even + wd.odd;
+            ordered_phase(v_cur, 0, k_nxt, 0, sc, sn, tile * C::kTileTokens + 32, mask_tag, [&](auto i) {
+                if constexpr (decltype(i)::value < TileWidener<D, E>::kPieces) wd.template store_piece<decltype(i)::value>(raw, scale, even, odd);
+            });
+            ordered_phase(v_cur, 1, k_nxt, 1, sn, sc, (tile + 1) * C::kTileTokens, mask_tag, [](auto) {});
+        }
         if (NEXT && copier) {
             copies_landed(j);
             if (!KVQ && decltype(mask_tag)::value && (tile + 2) * C::kTileTokens > kv_len)
@@ -997,13 +1085,14 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         // other loop wait for all copies in flight, and 17 tokens at 6966 beside 6 decodes take 53 us a layer instead of 47.)
         if constexpr (KVQ) {
             wait_loads_but<TileWidener<D, E>::kLoads>();
-            next_of_widener(0);
+            read_raw(0);
         } else if (copier) wait_loads_but<(NS + VS - 4) * C::kRuns>();
         for (int j = 0; j < n_sweep; j++) {
             if constexpr (KVQ) barrier_lds();
             else __syncthreads();
             if (copier && j + 1 < n_sweep) {
                 copies(j);
+                if constexpr (KVQ) wd.store(raw, raw_exponent, v0 == 0 ? VS - 1 : v0 - 1);
                 copies_landed(j);
                 s0 = s0 == NS - 1 ? 0 : s0 + 1;
                 v0 = v0 == VS - 1 ? 0 : v0 + 1;
@@ -1030,7 +1119,7 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         const int n_plain = max(0, min(n_sweep - 1, (wave_pmin + 1) / C::kTileTokens - t_begin - 1));
         if constexpr (KVQ) {  // tile 2, for step 0, and the page id of its fetch
             wait_loads_but<TileWidener<D, E>::kLoads>();
-            next_of_widener(0);
+            read_raw(0);
         } else if (copier) wait_loads_but<(NS + VS - 4) * C::kRuns>();  // K(1), for step 0; the others are waited for in its end
         int j = 0;
         for (; j < n_plain; j++) step(j, no, yes);
@@ -1923,11 +2012,11 @@ static int allow_prefill_lds(int device) {
                                    PrefillLds<D, NW, E::kKvq>::kBytes);
     };
     const Int<kMixedWaves> large;
-    for (hipError_t e : {allow(large, Int<0>()), allow(large, Int<1>()), allow(large, Int<2>())})
+    for (hipError_t e : {allow(large, Int<0>()), allow(large, Int<1>())})
         if (e != hipSuccess) return (int)e;
     if constexpr (!E::kKvq) {
         const Int<kSmallWaves> small;
-        for (hipError_t e : {allow(small, Int<0>()), allow(small, Int<1>())})
+        for (hipError_t e : {allow(large, Int<2>()), allow(small, Int<0>()), allow(small, Int<1>())})
             if (e != hipSuccess) return (int)e;
     }
     if (known) done[device].store(true, std::memory_order_release);
@@ -1958,8 +2047,9 @@ static int launch_attention_d(const tc_plan *p, const AttnArgs &A, int launches,
         const Int<kMixedWaves> large;
         const Int<kSmallWaves> small;
         const int wide = p->waves_per_item > 1 ? p->items_per_wg : 0;
-        if (E::kKvq || p->prefill_waves == kMixedWaves) wide == 2 ? launch(large, Int<2>()) : wide == 1 ? launch(large, Int<1>()) : launch(large, Int<0>());
-        else if constexpr (!E::kKvq) wide ? launch(small, Int<1>()) : launch(small, Int<0>());
+        if constexpr (E::kKvq) wide ? launch(large, Int<1>()) : launch(large, Int<0>());  // (the plan has no other form for it)
+        else if (p->prefill_waves == kMixedWaves) wide == 2 ? launch(large, Int<2>()) : wide == 1 ? launch(large, Int<1>()) : launch(large, Int<0>());
+        else wide ? launch(small, Int<1>()) : launch(small, Int<0>());
     } else if (grid > 0 && p->waves_per_item > 1) {
         static_assert(decode_lds_bytes(kWideWaves, 16, D) <= 65536, "more than 64 KiB of dynamic LDS needs an opt-in");
         auto launch = [&](auto per_wg) {

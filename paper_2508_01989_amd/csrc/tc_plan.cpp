@@ -731,7 +731,7 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
             p->items_per_wg = 1;
             p->waves_per_item = p->prefill_waves;
             const int64_t free_units = kNumCu - (int64_t)n_wg_head * Hkv;
-            if (!queue && p->prefill_waves == kMixedWaves && free_units >= kNumCu / 4)
+            if (!kvq && !queue && p->prefill_waves == kMixedWaves && free_units >= kNumCu / 4)
                 if (const int two = two_split_workgroups(p, S, split, free_units, false)) {
                     p->split_tokens = two;
                     p->items_per_wg = 2;
