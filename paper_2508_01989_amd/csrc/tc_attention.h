@@ -999,22 +999,28 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
     // One step for tile t_begin + j, which lives in stages s0 = j mod NS and v0 = j mod VS: `sc` holds the scores of its
     // first half, `kf` the K fragments of its second half.  NEXT: tile j + 1 exists.
     int s0 = 0, v0 = 0;
-    // A cache in 8 bits: what the step after needs of LDS, requested before its barrier: the page in raw stage `stage`, its exponent, the page id of the next fetch.
-    [[maybe_unused]] auto read_raw = [&](int stage) {
+    // A cache in 8 bits: what step j needs of LDS to widen its page, requested (the first products run until it is there), and the fetch of the page two steps on, when it has been used.
+    [[maybe_unused]] auto take_raw = [&](int j) {
         if constexpr (KVQ) {
+            wd.read(j & 1, lane, raw);
+            raw_exponent = wd.exponent(j & 1);
             id_next[0] = *reinterpret_cast<const int *>(wd.id_slot() + 4 * lane);
-            raw_exponent = wd.exponent(stage);
-            wd.read(stage, lane, raw);
+            const int n_valid = kv_len - ((t_begin + j + 2) * C::kTilePages + pg) * kBlock;
+            const bool diag = j + 2 < n_sweep && diagonal(t_begin + j + 2);
+            if (wd.is_v && (n_valid < kBlock || diag)) wd.clean(raw, n_valid, diag, lane);
         }
     };
-    [[maybe_unused]] auto tokens_of_raw = [&](int j) { return kv_len - ((t_begin + j + 2) * C::kTilePages + pg) * kBlock; };  // real ones, of the page widened in step j
-    auto copies = [&](int j) {  // K(j+NS) replaces K(j), V(j+VS-1) replaces V(j-1)
-        const int vm1 = v0 == 0 ? VS - 1 : v0 - 1;
-        if constexpr (KVQ) {  // tile j + 2 replaces tile j - 1 (past the end of the range the tile is never read)
+    [[maybe_unused]] auto fetch_next = [&](int j) {
+        if constexpr (KVQ) {
+            wd.reads_done();
             page_id_fetch(pages + page_index(t_begin + j + 5), wd.id_slot());
             wd.fetch(id_next[0], j & 1);
-            wd.clean(raw, tokens_of_raw(j), j + 2 < n_sweep && diagonal(t_begin + j + 2), lane);
-        } else if constexpr (NW == kMixedWaves) {
+        }
+    };
+    auto copies = [&](int j) {  // K(j+NS) replaces K(j), V(j+VS-1) replaces V(j-1)
+        const int vm1 = v0 == 0 ? VS - 1 : v0 - 1;
+        if constexpr (KVQ) take_raw(j);  // tile j + 2 replaces tile j - 1 (past the end of the range the tile is never read)
+        else if constexpr (NW == kMixedWaves) {
             // First the page ids for the next step's copies.  They are counted by vmcnt like the copies.
             page_id_fetch(pages + page_index(t_begin + j + 1 + NS), idk_slot);
             page_id_fetch(pages + page_index(t_begin + j + 1 + VS - 1), idv_slot);
@@ -1029,7 +1035,6 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         if constexpr (KVQ) wait_loads_but<TileWidener<D, E>::kLoads>();
         else wait_loads_but<VS == 3 ? 2 * C::kRuns : C::kRuns>();
         if constexpr (KVQ) {
-            read_raw((j + 1) & 1);
         } else if constexpr (NW == kMixedWaves) {
             id_next[2] = page_id_read(idk_slot, lane);
             id_next[VS - 2] = page_id_read(idv_slot, lane);
@@ -1064,11 +1069,12 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         if constexpr (!KVQ) phases();
         else if constexpr (!NEXT) phases();
         else {
-            const float scale = wd.scale(raw_exponent);
             char *const even = wd.even_piece(v0 == 0 ? VS - 1 : v0 - 1), *const odd = even + wd.odd;
-            ordered_phase(v_cur, 0, k_nxt, 0, sc, sn, tile * C::kTileTokens + 32, mask_tag, [&](auto i) {
-                if constexpr (decltype(i)::value < TileWidener<D, E>::kPieces) wd.template store_piece<decltype(i)::value>(raw, scale, even, odd);
+            ordered_phase(v_cur, 0, k_nxt, 0, sc, sn, tile * C::kTileTokens + 32, mask_tag, [&](auto g) {
+                constexpr int i = decltype(g)::value - (D == 128 ? 3 : 2);
+                if constexpr (i >= 0 && i < TileWidener<D, E>::kPieces) wd.template store_piece<i>(raw, wd.scale(raw_exponent), even, odd);
             });
+            fetch_next(j);
             ordered_phase(v_cur, 1, k_nxt, 1, sn, sc, (tile + 1) * C::kTileTokens, mask_tag, [](auto) {});
         }
         if (NEXT && copier) {
@@ -1085,14 +1091,16 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         // other loop wait for all copies in flight, and 17 tokens at 6966 beside 6 decodes take 53 us a layer instead of 47.)
         if constexpr (KVQ) {
             wait_loads_but<TileWidener<D, E>::kLoads>();
-            read_raw(0);
         } else if (copier) wait_loads_but<(NS + VS - 4) * C::kRuns>();
         for (int j = 0; j < n_sweep; j++) {
             if constexpr (KVQ) barrier_lds();
             else __syncthreads();
             if (copier && j + 1 < n_sweep) {
                 copies(j);
-                if constexpr (KVQ) wd.store(raw, raw_exponent, v0 == 0 ? VS - 1 : v0 - 1);
+                if constexpr (KVQ) {
+                    wd.store(raw, raw_exponent, v0 == 0 ? VS - 1 : v0 - 1);
+                    fetch_next(j);
+                }
                 copies_landed(j);
                 s0 = s0 == NS - 1 ? 0 : s0 + 1;
                 v0 = v0 == VS - 1 ? 0 : v0 + 1;
@@ -1119,7 +1127,6 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         const int n_plain = max(0, min(n_sweep - 1, (wave_pmin + 1) / C::kTileTokens - t_begin - 1));
         if constexpr (KVQ) {  // tile 2, for step 0, and the page id of its fetch
             wait_loads_but<TileWidener<D, E>::kLoads>();
-            read_raw(0);
         } else if (copier) wait_loads_but<(NS + VS - 4) * C::kRuns>();  // K(1), for step 0; the others are waited for in its end
         int j = 0;
         for (; j < n_plain; j++) step(j, no, yes);
