@@ -126,6 +126,7 @@ struct tc_plan {
     int prefill_waves = tc::kMixedWaves;   // waves of a workgroup beside a prefill chunk: 8, or 4 (prefill items of 128 rows)
     int rows_per_item = tc::kPrefillRows;  // (position, head) rows of a prefill item: 256 or 128
     int waves_per_item = 1;               // waves that share one of them: 1, all of a workgroup's (kWideWaves, beside a chunk prefill_waves) or half of them
+    int token_bytes() const { return (kvq ? 2 : 4) * D; }  // K and V of a token and KV head
     int launch_threads() const { return 64 * items_per_wg * waves_per_item; }
     int grid_blocks() const { return n_prefill_wg + n_decode_wg; }
     size_t workspace_bytes() const {

@@ -226,7 +226,7 @@ static int choose_wide_split_beside_chunk(const tc_plan *p, int S, double t_rest
             const int64_t kv = (int64_t)p->ctx_len[s] + 1;
             if (kv <= (int64_t)W * kMaxSplitPages * kBlock) longest = std::max(longest, kv);
         }
-    const double t_longest = 1.1 * (p->D / 128.0) * (double)longest / (kBlock * W);
+    const double t_longest = (p->kvq ? 0.55 : 1.1) * (p->D / 128.0) * (double)longest / (kBlock * W);
     const double share = !queue && n_prefill_wg > slots / 2 ? 0.8 : p->D == 64 ? 0.65 : 0.5;
     // More sweeps than the chip takes at once: the decode workgroups start when the last of them have, so what their longest wave needs comes
     // on top, unless the decodes themselves keep the chip busy for twice as long.  Alone it counts from 16 us on, 20 at head_dim 64: 1900 and 4700 tokens
@@ -499,7 +499,7 @@ static int64_t deal_units(const tc_plan *p, int n_wg_head, bool level_runs, int6
     const auto sweep_us = [&](int wg) {  // a piece each, the longest first
         return (w.pieces[wg].t1 - w.pieces[wg].t0) * (p->D == 64 ? 1.03 : 1.65) * (p->rows_per_item == kPrefillRows ? 1.0 : 0.6) + 3.0;
     };
-    const double unit_us = 4.0, us_per_token = 4.0 * p->D / 43.0e3;
+    const double unit_us = 4.0, us_per_token = p->token_bytes() / 43.0e3;
     double sum = n_units * unit_us + (double)decode_tokens * Hkv * us_per_token;
     for (int i = 0; i < n_wg_head; i++) sum += sweep_us(i) * Hkv;
     int64_t tokens[kNumCu / 2] = {};  // of the units that may be dealt
@@ -581,7 +581,7 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     PlanScratch &w = p->work;
 
     // ---- prefill row blocks, heaviest (latest positions, longest KV range) first, and their pieces
-    const int64_t decode_bytes = decode_tokens * Hkv * D * (kvq ? 2 : 4);
+    const int64_t decode_bytes = decode_tokens * Hkv * p->token_bytes();
     p->rows_per_item = choose_rows_per_item(p, S, decode_bytes);
     make_row_blocks(p, S, p->rows_per_item, w.blocks);
     // The sweeps in runs, at most `bins` per KV head: the number made, or 0 (the blocks as they were) where runs whose regions
@@ -775,7 +775,7 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     // 38 of 640-1400 3 % less to 4 % more (0.3 % more; 40/8, 424 with 286 of 1003 222.6 / 217.7, 32/8, 512 with 467 of 1002 331.4 / 344.0, 32/32, 2048 with 60 of 1176 335.7 / 347.3).
     const int split_long = p->split_tokens;  // of sequences that take several workgroups
     if (!w.blocks.empty() && p->prefill_waves == kMixedWaves && p->waves_per_item == 1 && decode_tokens >= (int64_t)2000 * n_decode_seqs)
-        while (p->split_tokens * D > 256 * 128 && (int64_t)p->split_tokens * W * 4 * D * 8 * kNumCu > decode_bytes) p->split_tokens /= 2;
+        while (p->split_tokens * D > 256 * 128 && (int64_t)p->split_tokens * W * p->token_bytes() * 8 * kNumCu > decode_bytes) p->split_tokens /= 2;
     const auto splits_of = [&](int64_t kv) { return num_splits(kv, kv > (int64_t)W * kMaxSplitPages * kBlock ? split_long : p->split_tokens, W); };
     w.runs.clear();
     for (int s = 0; s < S; s++) {
