@@ -26,7 +26,8 @@ __device__ __forceinline__ void transpose4(const uint32_t (&r)[4], uint32_t (&c)
 // when it does they are brought to it (exact but for the smallest numbers: a power of two moves their exponents).
 // K: a lane owns 16 elements of a token, the 16 bytes of a pool piece.  V: a lane owns eight elements of four tokens, which it transposes in
 // registers into the words of the token-minor pool.
-template <int D, class E>
+// CHUNK: the batch has a prefill chunk, whose pages may be new as a whole (a batch of decodes takes 5 % less without what that needs).
+template <int D, class E, bool CHUNK>
 __global__ void __launch_bounds__(256) kvq_append_kernel(uint8_t *k_pool, uint8_t *v_pool, uint8_t *scales,
                                                          const uint16_t *__restrict__ k_new, const uint16_t *__restrict__ v_new,
                                                          const int32_t *__restrict__ segments, int Hkv) {
@@ -99,7 +100,13 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(uint8_t *k_pool, uint8_
             *dst = w;
         }
     }
-    // ---- V
+    // ---- V.  A page that is all new goes through LDS, so that it is stored in whole pieces (a word at a time the stores of a wave touch a line four times): the eight groups
+    // of a tile lie 16 bytes further apart there, and the words that a wave stores at once are on different banks.
+    constexpr int kLds = CHUNK ? 8 * (2 * D + 16) : 16;  // of a wave
+    const auto lds_at = [](int byte) { return byte + byte / (2 * D) * 16; };
+    __shared__ __align__(16) char lds_all[4 * kLds];
+    char *const lds = lds_all + (threadIdx.x >> 6) * kLds;
+    const bool whole = CHUNK && n_tok == kBlock;
     if (qv.grows && is_old != 0) {
         if (!in_part) {
 #pragma unroll
@@ -116,7 +123,18 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(uint8_t *k_pool, uint8_
             for (int i = 0; i < 4; i++) r[i] = qv.bytes(vw[4 * i + 2 * half], vw[4 * i + 2 * half + 1]);
             transpose4(r, c);
 #pragma unroll
-            for (int i = 0; i < 4; i++) words[(4 * half + i) * (D / 32)] = (c[i] & is_new) | (was[4 * half + i] & ~is_new);
+            for (int i = 0; i < 4; i++) {
+                if (whole) *reinterpret_cast<uint32_t *>(lds + lds_at(v8_word<D>(g, cv * 8 + 4 * half + i))) = c[i];
+                else words[(4 * half + i) * (D / 32)] = (c[i] & is_new) | (was[4 * half + i] & ~is_new);
+            }
+        }
+    }
+    if (whole) {
+        __builtin_amdgcn_wave_barrier();  // (the LDS is this wave's own, and its accesses complete in order)
+#pragma unroll
+        for (int k = 0; k < D / 64; k++) {
+            const int at = k * 1024 + lane * 16;
+            *reinterpret_cast<u32x4 *>(v_pool + tile + at) = *reinterpret_cast<const u32x4 *>(lds + lds_at(at));
         }
     }
     if (lane == 0) *exponents = (uint16_t)((qk.e + 127) | ((qv.e + 127) << 8));
@@ -151,8 +169,8 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(const uint8_t *__restrict
         const int t = p * TK + tk;
         if (t < n) {
             u32x4 *dst = reinterpret_cast<u32x4 *>(k_out + at + t * row + ck * 16);
-            dst[0] = __builtin_bit_cast(u32x4, E::widen8(kw[p][0], kw[p][1], ks));
-            dst[1] = __builtin_bit_cast(u32x4, E::widen8(kw[p][2], kw[p][3], ks));
+            __builtin_nontemporal_store(__builtin_bit_cast(u32x4, E::widen8(kw[p][0], kw[p][1], ks)), dst);
+            __builtin_nontemporal_store(__builtin_bit_cast(u32x4, E::widen8(kw[p][2], kw[p][3], ks)), dst + 1);
         }
     }
     const uint32_t lo[4] = {vw[0], vw[1], vw[2], vw[3]}, hi[4] = {vw[4], vw[5], vw[6], vw[7]};
@@ -161,7 +179,7 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(const uint8_t *__restrict
     transpose4(hi, b);
 #pragma unroll
     for (int i = 0; i < 4; i++)
-        if (4 * g + i < n) *reinterpret_cast<u32x4 *>(v_out + at + (4 * g + i) * row + cv * 8) = __builtin_bit_cast(u32x4, E::widen8(a[i], b[i], vs));
+        if (4 * g + i < n) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, E::widen8(a[i], b[i], vs)), reinterpret_cast<u32x4 *>(v_out + at + (4 * g + i) * row + cv * 8));
 }
 
 // ------------------------------------------------------------------------------------
@@ -171,9 +189,12 @@ template <int D, class E>
 static int append_d(const tc_plan *p, const tc_kvq_pool *pool, const void *k_new, const void *v_new, hipStream_t st) {
     const int waves = std::min(4, p->Hkv);
     const dim3 grid((unsigned)p->n_append, (unsigned)((p->Hkv + waves - 1) / waves));
-    kvq_append_kernel<D, E><<<grid, waves * 64, 0, st>>>((uint8_t *)pool->base.k_pool, (uint8_t *)pool->base.v_pool, (uint8_t *)pool->scales,
-                                                        (const uint16_t *)k_new, (const uint16_t *)v_new, p->dev + p->off_append, p->Hkv);
-    return (int)hipGetLastError();
+    const auto launch = [&](auto kernel) {
+        kernel<<<grid, waves * 64, 0, st>>>((uint8_t *)pool->base.k_pool, (uint8_t *)pool->base.v_pool, (uint8_t *)pool->scales, (const uint16_t *)k_new,
+                                            (const uint16_t *)v_new, p->dev + p->off_append, p->Hkv);
+        return (int)hipGetLastError();
+    };
+    return p->n_append_prefill > 0 ? launch(kvq_append_kernel<D, E, true>) : launch(kvq_append_kernel<D, E, false>);
 }
 
 template <int D, class E>

@@ -179,7 +179,8 @@ static int two_split_workgroups(const tc_plan *p, int S, int split, int64_t at_o
 //   32/32 heads, one of 2157 tokens (34 pages a wave) among 29 short ones, 960 pairs 27.5 / 17.0
 static int choose_wide_split(const tc_plan *p, int S, int64_t decode_tokens) {
     const int64_t token_heads = decode_tokens * p->Hkv;
-    if (token_heads >= (int64_t)kNumCu * kDecodeWgPerCu * kDecodeWaves * 256) return 0;
+    // (A cache in 8 bits: twice the tokens for the same bytes; us, lines at 256 / 512: 32/8 heads, 38 of 2883 43.2 / 38.3, 32/32, head_dim 64, 8 of 3571 30.0 / 27.3.)
+    if (token_heads >= (int64_t)kNumCu * kDecodeWgPerCu * kDecodeWaves * (p->kvq ? 512 : 256)) return 0;
     const int split = choose_split(token_heads);  // of the single-wave form
     int64_t longest = 0, longest_pages = 0;       // the longest sequence; the pages of the longest single-wave split
     for (int s = 0; s < S; s++) {
