@@ -2,7 +2,9 @@
 prefills (paper Sec. 3.4, Algorithm 2), the per-iteration decode flow between instance types (Sec. 3.3,
 Algorithm 1), and KV migration between the instances' pools (Sec. 3.5) — all on one GPU, with the
 attention of every iteration computed by tc_kv_append / tc_mixed_attention and every migration by
-tc_kv_export / tc_kv_import.
+tc_kv_export / tc_kv_import.  An instance may hold its KV cache in 8 bits (`kvq`): its iterations are
+tc_kvq_mixed_attention_append, and a request moves to or from it as the rows its cache stands for
+(tc_kvq_read or tc_kv_gather, then the append of the other side).
 
 There is no model here: a request carries pre-drawn per-layer q / k / v rows for each of its positions
 (what the projections of a real model would produce), so the loop is teacher-forced and its attention
@@ -16,7 +18,8 @@ from dataclasses import dataclass, field
 import numpy as np
 import torch
 
-from . import Plan, make_pool, tc_kv_append, tc_kv_export, tc_kv_import, tc_kv_transfer_bytes, tc_mixed_attention
+from . import (Plan, make_kvq_pool, make_pool, tc_kv_append, tc_kv_export, tc_kv_gather, tc_kv_import, tc_kv_transfer_bytes,
+               tc_kvq_append, tc_kvq_mixed_attention_append, tc_kvq_read, tc_mixed_attention)
 from . import sched
 
 BLOCK = 16
@@ -52,13 +55,19 @@ class Request:
 
 
 class Instance:
-    def __init__(self, index, kind, chunk, num_blocks, shape, layers, device="cuda:0", dry=False):
+    def __init__(self, index, kind, chunk, num_blocks, shape, layers, device="cuda:0", dry=False, kvq=False):
         self.index, self.kind, self.chunk, self.num_blocks = index, kind, chunk, num_blocks
         self.Hq, self.Hkv, self.D = shape
         self.layers = layers
         self.dry = dry  # scheduling and accounting only: no pools, no kernels (runs without a GPU)
-        if not dry:
-            n = num_blocks * self.Hkv * BLOCK * self.D
+        self.kvq = kvq  # the KV cache is held in 8 bits
+        n = num_blocks * self.Hkv * BLOCK * self.D
+        if not dry and kvq:
+            self.k_pools, self.v_pools = ([torch.zeros(n, dtype=torch.uint8, device=device) for _ in range(layers)] for _ in range(2))
+            self.scales = [torch.zeros(num_blocks * self.Hkv * 2, dtype=torch.uint8, device=device) for _ in range(layers)]
+            self.pools = [make_kvq_pool(self.Hq, self.Hkv, self.D, num_blocks, self.k_pools[l], self.v_pools[l], self.scales[l])
+                          for l in range(layers)]
+        elif not dry:
             self.k_pools = [torch.zeros(n, dtype=torch.int16, device=device) for _ in range(layers)]
             self.v_pools = [torch.zeros(n, dtype=torch.int16, device=device) for _ in range(layers)]
             self.pools = [make_pool(self.Hq, self.Hkv, self.D, num_blocks, self.k_pools[l], self.v_pools[l])
@@ -154,8 +163,11 @@ class Instance:
             q = torch.cat([r.q[l, a:b] for r, a, b in rows])
             k = torch.cat([r.k[l, a:b] for r, a, b in rows])
             v = torch.cat([r.v[l, a:b] for r, a, b in rows])
-            tc_kv_append(plan, self.pools[l], k, v)
-            tc_mixed_attention(plan, self.pools[l], q, out, scale, ws, plan.workspace_bytes)
+            if self.kvq:
+                tc_kvq_mixed_attention_append(plan, self.pools[l], q, k, v, out, scale, ws, plan.workspace_bytes)
+            else:
+                tc_kv_append(plan, self.pools[l], k, v)
+                tc_mixed_attention(plan, self.pools[l], q, out, scale, ws, plan.workspace_bytes)
             for i, (r, a, b) in enumerate(rows):
                 r.out[l, a:b] = out[int(q_start[i]):int(q_start[i + 1])]
         torch.cuda.synchronize()
@@ -188,11 +200,13 @@ class Instance:
 
 
 class Cluster:
-    """Proxy plus instances.  kinds / chunks / blocks: one entry per instance."""
+    """Proxy plus instances.  kinds / chunks / blocks: one entry per instance; kvq: one too, or the same for all."""
 
     def __init__(self, kinds, chunks, blocks, shape, layers, cm, tpot_slo, ttft_slo, alpha=0.96, watermark_frac=0.95,
-                 link_bytes_per_s=150e9, dry=False):
-        self.inst = [Instance(i, k, c, b, shape, layers, dry=dry) for i, (k, c, b) in enumerate(zip(kinds, chunks, blocks))]
+                 link_bytes_per_s=150e9, dry=False, kvq=False):
+        kvq = list(kvq) if isinstance(kvq, (list, tuple)) else [kvq] * len(kinds)
+        self.inst = [Instance(i, k, c, b, shape, layers, dry=dry, kvq=e)
+                     for i, (k, c, b, e) in enumerate(zip(kinds, chunks, blocks, kvq))]
         self.dry = dry
         self.cm, self.tpot_slo, self.ttft_slo, self.alpha = cm, tpot_slo, ttft_slo, alpha
         self.watermark_frac, self.link = watermark_frac, link_bytes_per_s
@@ -222,11 +236,14 @@ class Cluster:
         src = self.inst[req.where]
         kv = req.done
         Hq, Hkv, D = self.shape
-        nbytes = self.layers * ((kv + BLOCK - 1) // BLOCK) * 2 * Hkv * BLOCK * D * 2
+        by_pages = not (src.kvq or dst.kvq)  # else the rows the cache stands for, in 16 bits
+        nbytes = self.layers * ((kv + BLOCK - 1) // BLOCK * BLOCK if by_pages else kv) * 2 * Hkv * D * 2
         old = req.blocks
         req.blocks = []
         dst.reserve(req)
-        if not self.dry:
+        if not self.dry and not by_pages:
+            self._move_rows(src, dst, kv, old, req.blocks)
+        elif not self.dry:
             one = (np.array([0, 1], np.int32), np.array([kv - 1], np.int32))
             plan_s = Plan(src.pools[0], one[0], one[1], np.array([old], np.int32))
             assert nbytes == tc_kv_transfer_bytes(plan_s, 0, self.layers)
@@ -245,6 +262,20 @@ class Cluster:
         req.decode_start_time, req.decode_start_done = req.ready, req.done  # treated as a new decode request
         req.route.append((now, why, dst.index))
         self.stats["bytes_moved"] += nbytes
+
+    def _move_rows(self, src, dst, kv, src_blocks, dst_blocks):
+        """One request's rows out of the cache of `src` and into that of `dst`, either of them in 8 bits or in 16."""
+        _, Hkv, D = self.shape
+        plan_s = Plan(src.pools[0], np.array([0, 1], np.int32), np.array([kv - 1], np.int32), np.array([src_blocks], np.int32))
+        plan_d = Plan(dst.pools[0], np.array([0, kv], np.int32), np.zeros(1, np.int32), np.array([dst_blocks], np.int32))
+        k = torch.empty((kv, Hkv, D), dtype=torch.int16, device=src.device)
+        v = torch.empty_like(k)
+        for l in range(self.layers):
+            (tc_kvq_read if src.kvq else tc_kv_gather)(plan_s, src.pools[l], 0, k, v)
+            (tc_kvq_append if dst.kvq else tc_kv_append)(plan_d, dst.pools[l], k, v)
+        torch.cuda.synchronize()
+        plan_s.destroy()
+        plan_d.destroy()
 
     def _pick(self, want, need, stay=-1):
         return sched.pick_instance([x.kind for x in self.inst], [x.blocks_used for x in self.inst],
