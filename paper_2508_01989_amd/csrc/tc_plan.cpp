@@ -635,7 +635,12 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
             // levelled 143 / 155), and where the items nearly fill the chip beside decodes at all, whose queue levels too, only when the sweeps
             // are very uneven (1700 at 3000 with 32 of lognormal 1024 116.2 / 118.1; 8, 800 at 0 and 746 at 7226 with 21 of 1200 156.0 / 129.2),
             // without decodes not for a few per cent either (1500 at 20000, 40/8 heads, head_dim 64, 326 / 341).
-            const double level_below = items * 4 <= 3 * kNumCu ? 0.95 : decode_tokens > 0 ? 0.7 : 0.9;
+            double level_below = items * 4 <= 3 * kNumCu ? 0.95 : decode_tokens > 0 ? 0.7 : 0.9;
+            // In 8 bits a level run costs less beside whole items than the estimates say, up to an item per unit in any batch and at head_dim 128 beyond it
+            // (whole / levelled, us: 32/8 heads, 2048 at 0 54.2 / 49.5, 1842 at 0 48.5 / 42.4; 16/2, 1207 at 0 33.9 / 30.1, 1456 at 0 with 60 decodes
+            // 40.4 / 29.9; head_dim 64, 40/8, 1516 at 0 30.1 / 25.5; over an item per unit at head_dim 64 28/4, 3938 and 2363 at 0 97.5 / 108).  Of 96 batches that
+            // this line and one of 1.25 decide differently those between the two were as often slower levelled (by up to 13 %) as faster.
+            if (kvq && (items * 4 <= 3 * kNumCu || (decode_tokens == 0 && (D == 128 || items <= kNumCu)))) level_below = 1.05;
             // Small workgroups: beside more decodes the queue fills the units whose sweeps end early; long sweeps run at a lower clock in either
             // form than the estimates say (6562 at 16848, 8/8 heads, 526 / 543).
             const double small_below = (w.blocks[0].n_tiles <= 64 ? 0.97 : 0.9) * t_whole;
