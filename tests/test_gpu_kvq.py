@@ -5,6 +5,7 @@ The bound: probabilities and outputs are rounded to nearest in the element type 
 held in 32 bits.  With a = sum_j p_j |v_j| / sum_j p_j the rounding of p moves an output by at most h a and its own rounding by at
 most h |out|.  A probability of IEEE half below 2^-14 of the reference is rounded in steps of 2^-24 instead, which adds at most 2^-25 |v|
 per key, and the probabilities' sum is at least about one.  32-bit arithmetic (score products, exponentials, sums) adds less than a fiftieth of h."""
+import copy
 import zlib
 
 import numpy as np
@@ -270,6 +271,100 @@ def test_every_pattern_is_quantised_and_read_back(tc, dtype):
     for s in range(c.S):
         for x, y in zip(dev.read(s), cache.read(c.table[s], int(c.kv[s]))):
             assert np.array_equal(x, y, equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("S,Hq,Hkv", [(6, 8, 2), (240, 32, 8)])  # a split is run by a workgroup, by a wave
+def test_new_tokens_of_decodes_at_the_ends_of_the_range(tc, S, Hq, Hkv, dtype):
+    """Decodes whose new row is as large or as small as the type allows, or has infinities and NaN beside such numbers: the cache that the attention
+    launch leaves, and NaN in the outputs."""
+    c = Case(f"ends {S}", Hq, Hkv, 64, [1] * S, [(5 * i) % 50 + (i % 3 == 0) * 16 for i in range(S)], dtype=dtype)
+    big, inf, nan = (0x7BFF, 0x7C00, 0x7E01) if dtype == "fp16" else (0x7F7F, 0x7F80, 0x7FC1)
+    rng = np.random.default_rng(3)
+    for i in range(S):
+        for x in (c.k_new, c.v_new):
+            x[i] = {0: big, 1: 1, 2: big | 0x8000, 3: x[i], 4: 0, 5: x[i]}[i % 6]
+            if i % 6 == 0:
+                x[i, 0, ::3] = rng.integers(0, 65536, 22, dtype=np.uint16)
+            if i % 6 in (2, 5):
+                x[i, 1, [1, 62]] = inf, nan
+    print(f"[case] ends {S} {dtype}", flush=True)
+    cache = c.oracle_cache()
+    dev = Device(tc, c)
+    assert (dev.plan.info.waves_per_item == 1) == (S == 240)
+    dev.step()
+    check_cache(dev, cache, "step")
+    got = dev.outputs()
+    for i in range(S):
+        if i % 6 in (2, 5):  # (the query heads of KV head 1)
+            assert np.isnan(got[i, 4:8]).all()
+    plain = [i for i in range(S) if i % 6 in (1, 3, 4)]
+    ordinary = copy.copy(c)
+    ordinary.v_new = c.v_new[plain]  # (the bound of IEEE half is by the largest value)
+    want, bound = ordinary.attention(cache)
+    check_attention(got[plain], want[plain], bound[plain], "plain rows")
+    apart = Device(tc, c)
+    apart.append()
+    check_cache(apart, cache, "append")
+    apart.attention()
+    assert np.array_equal(apart.outputs(), got, equal_nan=True)
+
+
+def test_large_stream_of_decodes_in_one_call_and_in_two(tc):
+    """Half a gigabyte of pages, where the append is a launch of its own: the bits of the two calls."""
+    import torch
+    Hq, Hkv, D, S = 32, 8, 128, 520
+    rng = np.random.default_rng(21)
+    ctx = rng.integers(440, 560, S).astype(np.int32)
+    pages = -(-(ctx + 1) // 16)
+    n = int(pages.sum())
+    assert n * Hkv * 2 * 16 * D >= 500_000_000
+    table = np.zeros((S, int(pages.max())), np.int32)
+    ids, at = rng.permutation(n).astype(np.int32), 0
+    for i, x in enumerate(pages):
+        table[i, :x] = ids[at:at + x]
+        at += x
+    g = torch.Generator(device="cuda:0").manual_seed(5)
+    byte = lambda m, lo, hi: torch.randint(lo, hi, (m,), dtype=torch.uint8, device="cuda:0", generator=g)  # noqa: E731
+    pools = [byte(n * Hkv * 16 * D, 0, 0x7F) for _ in range(2)] + [byte(n * Hkv * 2, 115, 122)]
+    row = lambda h: torch.randn((S, h, D), device="cuda:0", generator=g).bfloat16()  # noqa: E731
+    q, k_new, v_new = row(Hq), row(Hkv), row(Hkv)
+    got = []
+    print("[case] large stream", flush=True)
+    for both in (False, True):
+        k, v, s = (x.clone() for x in pools)
+        pool = tc.make_kvq_pool(Hq, Hkv, D, n, k, v, s)
+        plan = tc.Plan(pool, np.arange(S + 1, dtype=np.int32), ctx, table)
+        assert plan.info.waves_per_item == 1
+        ws = torch.empty(max(16, plan.workspace_bytes), dtype=torch.uint8, device="cuda:0")
+        out = torch.empty((S, Hq, D), dtype=torch.bfloat16, device="cuda:0")
+        if both:
+            tc.tc_kvq_mixed_attention_append(plan, pool, q, k_new, v_new, out, D ** -0.5, ws)
+        else:
+            tc.tc_kvq_append(plan, pool, k_new, v_new)
+            tc.tc_kvq_mixed_attention(plan, pool, q, out, D ** -0.5, ws)
+        torch.cuda.synchronize()
+        got.append((k, v, s, out))
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+    assert torch.isfinite(got[0][3].float()).all() and not torch.equal(got[0][0], pools[0])
+
+
+def test_sequences_that_share_their_first_blocks(tc):
+    """The whole blocks of a common prompt may stand in several tables: nothing is appended to them."""
+    c = copy.copy(Case("shared", 8, 2, 128, [1, 1, 20], [100, 130, 97]))
+    c.k_hist, c.v_hist, c.table = c.k_hist.copy(), c.v_hist.copy(), c.table.copy()
+    for s in (1, 2):
+        c.table[s, :6] = c.table[0, :6]
+        for x in (c.k_hist, c.v_hist):
+            x[c.h_start[s]:c.h_start[s] + 96] = x[:96]
+    print("[case] shared blocks", flush=True)
+    cache = c.oracle_cache()
+    dev = Device(tc, c)
+    dev.step()
+    check_cache(dev, cache, "step")
+    want, bound = c.attention(cache)
+    check_attention(dev.outputs(), want, bound, "shared")
 
 
 def test_blocks_beyond_two_and_four_gigabytes(tc):
