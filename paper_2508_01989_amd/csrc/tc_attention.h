@@ -1,5 +1,27 @@
 // Device code of the mixed-batch attention kernels and their launch, templates over head_dim and the element type
 // (struct Bf16 and those after it).  tc_kernels.hip instantiates them for caches in 16 bits, tc_kvq.hip for caches in 8.
+//
+//   mixed_attention_kernel  ONE launch per layer for the whole mixed batch
+//       (paper Sec. 2.2: a prompt chunk plus piggybacked decodes share an iteration):
+//         workgroups [0, n_prefill)      causal chunked-prefill pieces: 8 (4) waves = 256 (128) (position, head) rows
+//                                        of one KV head over a range of 64-token KV tiles, MFMA 32x32x16,
+//                                        software-pipelined so that the softmax runs under the MFMAs
+//         remaining workgroups           one decode KV split per wavefront (splits of one sequence and KV head
+//                                        that share a workgroup are combined in LDS),
+//                                        MFMA 16x16x32 and 16x16x16
+//       Three shapes: 8 waves per workgroup, one workgroup per compute unit, when the batch has a prefill
+//       chunk, or 4 waves, two or three workgroups per compute unit, for chunks of uneven sweeps (each with a form
+//       that runs a decode split by a whole workgroup); 4 waves, three workgroups per
+//       compute unit, for a batch of decodes only.  Instantiated for bf16 and IEEE half.
+//   wide_decode_kernel the same for a batch of few decodes: a split is run by a workgroup of four waves
+//   split_merge_kernel combine the partial results of split decode sequences and of cut prefill row blocks
+//
+// Both attention branches compute S^T = K Q^T and O^T = V^T P^T so that the
+// probabilities a lane produces are exactly the B operand it must feed to the second
+// MFMA (no cross-lane movement), and the per-row softmax state is one scalar per lane.
+// The pool layouts (K: [D/8][16][8], V: [D][16] per block and KV head) are the MFMA
+// A-operand layouts of those two products, so K/V go from memory to the matrix cores
+// without any transposition.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -481,7 +503,8 @@ __device__ __forceinline__ void barrier_lds() {
 // A step or more later read() takes it back, 32 bytes a lane at head_dim 128 (16 at 64), and store_piece() leaves it in the tile's stage in 16 bits, in the layout that the
 // sweep reads: eight elements at a time, so that the sweep can put a piece under each of its first products.  A byte is
 // thus widened once per workgroup, two per instruction, and 16 KiB of a tile cross LDS once more; widened by every wave behind its
-// operand reads it would be eight times.
+// operand reads it would be eight times.  The widening runs under matrix products and costs a long sweep 7 % over one of tiles in 16 bits: 8192 tokens at 8192,
+// 64/8 heads, head_dim 128, 2.82 ms and 1.17 PFLOP/s (2.64 in 16 bits), 2048 at 4096 with 64 decodes, 32/8 heads, 173 us (169), each with the clock at the power limit.
 template <int D, class E>
 struct TileWidener {
     using C = PrefillCfg<D>;
@@ -1032,13 +1055,11 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         }
     };
     auto copies_landed = [&](int j) {  // those of the step before (two stages of V: this step's V too), and the page ids
-        if constexpr (KVQ) wait_loads_but<TileWidener<D, E>::kLoads>();
-        else wait_loads_but<VS == 3 ? 2 * C::kRuns : C::kRuns>();
-        if constexpr (KVQ) {
-        } else if constexpr (NW == kMixedWaves) {
+        wait_loads_but<KVQ ? TileWidener<D, E>::kLoads : VS == 3 ? 2 * C::kRuns : C::kRuns>();
+        if constexpr (!KVQ && NW == kMixedWaves) {
             id_next[2] = page_id_read(idk_slot, lane);
             id_next[VS - 2] = page_id_read(idv_slot, lane);
-        } else {
+        } else if constexpr (!KVQ) {
             const int t = j + 1 + NS;
             if ((t & 63) == 0) {
                 window = pages[page_index(t_begin + t + lane)];
@@ -1191,7 +1212,8 @@ struct DecodePage {  // K and V of one page, in MFMA A-operand registers
 };
 // The same of a cache in 8 bits.  A lane's 16 bytes of K are those of d = 16 (4 i + g) .. + 15 of token j, which make its operands of two
 // k-steps; its D/32 words of V those of tokens 4 g .. 4 g + 3 of d = 32 c + 16 i + j, one word per 16-row tile of O^T.
-// Half the registers of a page in 16 bits: twice as many pages in flight.
+// Half the registers of a page in 16 bits: more pages in flight.  Bound by the bytes of the pages, as in 16 bits, of which there are half: 512 sequences of 1000-3000
+// tokens, 32/8 heads, head_dim 128, 335 us and 6.37 TB/s (636 us in 16 bits), 256 of 512-4096 beside a chunk, 40/8, 207 (369), 2 of 16384-32768, 64/8, 22.1 (39.2).
 template <int D>
 struct DecodePage8 {
     typedef uint32_t piece __attribute__((ext_vector_type(D / 32)));

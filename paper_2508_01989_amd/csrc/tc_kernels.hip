@@ -3,27 +3,7 @@
 //   kv_append_kernel   scatter this iteration's K/V rows into the paged pools      (HBM-bound)
 //   kv_gather_kernel   un-paged copy of one sequence (test hook)                   (HBM-bound)
 //   kv_migrate_kernel  pool <-> contiguous transfer buffer, all layers (paper Sec. 3.5)   (HBM-bound)
-//   mixed_attention_kernel  ONE launch per layer for the whole mixed batch
-//       (paper Sec. 2.2: a prompt chunk plus piggybacked decodes share an iteration):
-//         workgroups [0, n_prefill)      causal chunked-prefill pieces: 8 (4) waves = 256 (128) (position, head) rows
-//                                        of one KV head over a range of 64-token KV tiles, MFMA 32x32x16,
-//                                        software-pipelined so that the softmax runs under the MFMAs
-//         remaining workgroups           one decode KV split per wavefront (splits of one sequence and KV head
-//                                        that share a workgroup are combined in LDS),
-//                                        MFMA 16x16x32 and 16x16x16
-//       Three shapes: 8 waves per workgroup, one workgroup per compute unit, when the batch has a prefill
-//       chunk, or 4 waves, two or three workgroups per compute unit, for chunks of uneven sweeps (each with a form
-//       that runs a decode split by a whole workgroup); 4 waves, three workgroups per
-//       compute unit, for a batch of decodes only.  Instantiated for bf16 and IEEE half.
-//   wide_decode_kernel the same for a batch of few decodes: a split is run by a workgroup of four waves
-//   split_merge_kernel combine the partial results of split decode sequences and of cut prefill row blocks
-//
-// Both attention branches compute S^T = K Q^T and O^T = V^T P^T so that the
-// probabilities a lane produces are exactly the B operand it must feed to the second
-// MFMA (no cross-lane movement), and the per-row softmax state is one scalar per lane.
-// The pool layouts (K: [D/8][16][8], V: [D][16] per block and KV head) are the MFMA
-// A-operand layouts of those two products, so K/V go from memory to the matrix cores
-// without any transposition.
+//   the attention kernels of tc_attention.h over pools in 16 bits, bf16 and IEEE half
 #include <cstdlib>
 
 #include "tc_attention.h"

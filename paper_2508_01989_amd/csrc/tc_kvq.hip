@@ -21,12 +21,17 @@ __device__ __forceinline__ void transpose4(const uint32_t (&r)[4], uint32_t (&c)
     c[2] = __builtin_amdgcn_perm(hi23, hi01, 0x05040100);
     c[3] = __builtin_amdgcn_perm(hi23, hi01, 0x07060302);
 }
+
 // A wave writes the rows that one sequence adds to one page (1..16 consecutive token indices) for one KV head: it alone writes the tile, so
 // it may read, change and write words of which a part is new.  Where the page has older rows, the exponent can only grow, and
 // when it does they are brought to it (exact but for the smallest numbers: a power of two moves their exponents).
 // K: a lane owns 16 elements of a token, the 16 bytes of a pool piece.  V: a lane owns eight elements of four tokens, which it transposes in
 // registers into the words of the token-minor pool.
 // CHUNK: the batch has a prefill chunk, whose pages may be new as a whole (a batch of decodes takes 5 % less without what that needs).
+// Bound: three bytes of memory traffic per new element, two of them read.  8192 tokens, 8 KV heads, head_dim 128 (50.4 MB) take
+// 10.1 us, 5.0 TB/s, what a plain copy of 2 GiB reaches.  Small batches are two accesses to memory one after the other, the segment and then everything else: 8
+// tokens 4.0 us, 512 tokens of 512 sequences 5.5 (5.0 back to back; with elements quantised one at a time 8.4).  A wave
+// to each (page, KV head) needs no barrier.
 template <int D, class E, bool CHUNK>
 __global__ void __launch_bounds__(256) kvq_append_kernel(uint8_t *k_pool, uint8_t *v_pool, uint8_t *scales,
                                                          const uint16_t *__restrict__ k_new, const uint16_t *__restrict__ v_new,
@@ -140,7 +145,9 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(uint8_t *k_pool, uint8_
     if (lane == 0) *exponents = (uint16_t)((qk.e + 127) | ((qv.e + 127) << 8));
 }
 
-// A wave reads one page of one KV head back: the tokens that are real, widened, at the rows they have in k_out / v_out.
+// A wave reads one page of one KV head back: the tokens that are real, widened, at the rows they have in k_out / v_out.  Widening is exact, one instruction for
+// two elements.  Bound: three bytes of traffic per element, two of them written; the outputs are streamed past the caches, which nothing reads soon.  16 sequences
+// of 34300 tokens in all, 8 KV heads, head_dim 128 (211 MB) 37.5 us, 5.6 TB/s (stores through the caches 47.8); one of 1550 tokens 3.8 us, a chain of three accesses.
 template <int D, class E>
 __global__ void __launch_bounds__(256) kvq_read_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict__ v_pool,
                                                        const uint8_t *__restrict__ scales, const int32_t *__restrict__ pages,
