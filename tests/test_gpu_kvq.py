@@ -539,3 +539,63 @@ def test_many_kv_heads(tc, Hq, Hkv, D):
     for s in range(c.S):
         for x, y in zip(dev.read(s), cache.read(c.table[s], int(c.kv[s]))):
             assert np.array_equal(x, y)
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_attention_equals_that_of_a_cache_in_16_bits_which_holds_what_is_read_back(tc, seed):
+    """Random batches of every form: append, attention, read, append to a cache in 16 bits, attention there.  Both attentions are over the same
+    numbers, so they differ by at most the sum of their bounds; the mean magnitude in them comes from the 16-bit attention over |v|."""
+    import random
+
+    import torch
+    rng, gen = random.Random(seed), torch.Generator(device="cuda:0").manual_seed(seed)
+    for i in range(25):
+        Hkv, G, D, dtype = rng.choice([1, 2, 3, 4, 8, 8]), rng.choice([1, 2, 3, 4, 5, 7, 8, 16]), rng.choice([64, 128]), rng.choice(["bf16", "fp16"])
+        batch = [(int(2 ** rng.uniform(1, 11)), rng.choice([0, int(2 ** rng.uniform(0, 12))])) for _ in range(rng.choice([0, 1, 1, 2, 3]))]
+        batch += [(1, int(2 ** rng.uniform(0, 11))) for _ in range(rng.choice([0, 1, 3, 10, 40, 200]))] or [(1, rng.randrange(30000))]
+        rng.shuffle(batch)
+        q_len, ctx = (np.array(x, np.int32) for x in zip(*batch))
+        print(f"[case] {seed}.{i} {G * Hkv}/{Hkv} d{D} {dtype} chunks {[b for b in batch if b[0] > 1]} decodes {int((q_len == 1).sum())}", flush=True)
+        kv = q_len + ctx
+        q_start, all_rows = (np.concatenate([[0], np.cumsum(x)]).astype(np.int32) for x in (q_len, kv))
+        pages = -(-kv // 16)
+        blocks = int(pages.sum()) + 2
+        ids, table, at = np.random.default_rng(i).permutation(blocks).astype(np.int32), np.zeros((len(kv), int(pages.max())), np.int32), 0
+        for s, n in enumerate(pages):
+            table[s, :n] = ids[at:at + n]
+            at += n
+        Hq, n, code = G * Hkv, blocks * Hkv * 16 * D, tc.TC_FP16 if dtype == "fp16" else tc.TC_BF16
+        T = torch.float16 if dtype == "fp16" else torch.bfloat16
+        row = lambda m, h: torch.randn((m, h, D), device="cuda:0", generator=gen).to(T)  # noqa: E731
+        fill = lambda m, x, t: torch.full((m,), x, dtype=t, device="cuda:0")  # noqa: E731
+        k8, v8, scales = fill(n, 0x7F, torch.uint8), fill(n, 0x7F, torch.uint8), fill(blocks * Hkv * 2, 0xFF, torch.uint8)
+        k16, v16, v_abs = (fill(n, -1, torch.int16) for _ in range(3))
+        pool = tc.make_kvq_pool(Hq, Hkv, D, blocks, k8, v8, scales, dtype=code)
+        pool16, absolute = (tc.make_pool(Hq, Hkv, D, blocks, k16, x, dtype=code) for x in (v16, v_abs))
+        old = np.flatnonzero(ctx > 0)
+        if len(old):
+            start = np.concatenate([[0], np.cumsum(ctx[old])]).astype(np.int32)
+            history = tc.Plan(pool, start, np.zeros(len(old), np.int32), table[old])
+            tc.tc_kvq_append(history, pool, row(int(start[-1]), Hkv), row(int(start[-1]), Hkv))
+            torch.cuda.synchronize()
+        m, total, scale = int(q_start[-1]), int(kv.sum()), D ** -0.5
+        q, k_new, v_new = row(m, Hq), row(m, Hkv), row(m, Hkv)
+        plan = tc.Plan(pool, q_start, ctx, table)
+        ws = fill(max(16, plan.workspace_bytes), 0xAB, torch.uint8)
+        out, want, mean = (torch.empty((m, Hq, D), dtype=T, device="cuda:0") for _ in range(3))
+        tc.tc_kvq_mixed_attention_append(plan, pool, q, k_new, v_new, out, scale, ws)
+        k, v = (torch.empty((total, Hkv, D), dtype=T, device="cuda:0") for _ in range(2))
+        tc.tc_kvq_read(plan, pool, -1, k, v)
+        whole, plan16 = tc.Plan(pool16, all_rows, np.zeros(len(kv), np.int32), table), tc.Plan(pool16, q_start, ctx, table)
+        tc.tc_kv_append(whole, pool16, k, v)
+        v_abs.copy_(v16 & 0x7FFF)
+        ws16 = fill(max(16, plan16.workspace_bytes), 0xAB, torch.uint8)
+        tc.tc_mixed_attention(plan16, pool16, q, want, scale, ws16)
+        tc.tc_mixed_attention(plan16, absolute, q, mean, scale, ws16)
+        torch.cuda.synchronize()
+        h = HALF_STEP[dtype]
+        bound = 2 * h * 1.02 * (mean.double() * (1 + 3 * h) + want.double().abs() * (1 + h))
+        if dtype == "fp16":
+            bound += 2 * int(kv.max()) * 2.0 ** -25 * v.double().abs().max()
+        over = ((out.double() - want.double()).abs() / (bound + 1e-30)).max().item()
+        assert over <= 1.0, over
