@@ -239,7 +239,10 @@ static int choose_wide_split_beside_chunk(const tc_plan *p, int S, double t_rest
     // 8344 at 65, 2 of 2400-9500) 2013 / 1969.  Long decode streams: 40/8 heads, 2664 at 0 with 29 of 2600-10400 (160 us of K/V) 216.7 / 226.1, 3136
     // at 0 with 31 of 3800-15400 315.9 / 327.2; 32/8, 10816 at 4394 with 34 of 3600-14400 1590 / 1613.
     const bool late = !queue && n_prefill_wg > slots;
-    const double t_rest = std::max(t_rest_us, 8.0);
+    // What else the launch takes at the least: a start and an end.  In 8 bits, whose pages go by twice as fast, waves that wait for one page after the other are what a small
+    // batch waits for sooner (us, a line of 8 / this one: 8/8 heads, 6 at 27 with one of 1291 6.7 / 5.7, 40/8, 5 at 0 with 23 of 548 8.1 / 6.1, 28/4, 6 at 0 with 25 of 166 7.1 / 5.7;
+    // head_dim 64, 8/8, 6 at 0 with 2 of 2981 8.0 / 6.1, 40/8, 3 at 43 with 3 of 2914 8.1 / 6.3, but a line of 3 there, 8/8, 6 at 5 with 17 of 1164 6.1 / 6.4).
+    const double t_rest = std::max(t_rest_us, !p->kvq ? 8.0 : p->D == 64 ? 4.0 : 1.0);
     const double line = late ? std::max(std::min(share * t_rest, p->D == 64 ? 20.0 : 16.0), 0.5 * t_decode_us) : share * t_rest;
     if (t_longest <= line) return 0;
     const int split = shortest_split(p, S, std::max<int64_t>(slots - n_prefill_wg, slots / 4));
