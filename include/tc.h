@@ -258,7 +258,7 @@ typedef struct {
  * element x becomes the E4M3 number nearest to x * 2^-e (ties to even; where limited, the largest); infinities and NaN become
  * NaN.  Where e grows, the block's earlier rows are brought to it the same way, which changes only numbers below 2^-6 of the
  * new scale.  What a block holds beyond the sequence's last token is left as it was.  A block that gets rows must belong
- * to one sequence of the batch only; what the call leaves depends on the rows and the cache alone, and making it again changes
+ * to one sequence of the batch only (TC_ERR_BLOCK if two sequences would put rows into the same one); what the call leaves depends on the rows and the cache alone, and making it again changes
  * nothing. */
 tc_status tc_kvq_append(const tc_plan *plan, const tc_kvq_pool *pool, const void *k_new, const void *v_new, void *stream);
 

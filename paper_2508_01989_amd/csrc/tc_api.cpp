@@ -200,7 +200,8 @@ tc_status check_kvq_device(const tc_plan *plan) {  // last, so that a plan witho
     return TC_OK;
 }
 
-tc_status check_kvq_rows(const void *k_new, const void *v_new) {
+tc_status check_kvq_rows(const tc_plan *plan, const void *k_new, const void *v_new) {
+    if (plan->append_shared) return fail(TC_ERR_BLOCK, "a block gets rows from more than one place of the block table");
     if (!k_new || !v_new) return fail(TC_ERR_NULL, "k_new or v_new is NULL");
     if (misaligned(k_new, 16) || misaligned(v_new, 16)) return fail(TC_ERR_ARG, "k_new and v_new must be 16-byte aligned");
     return TC_OK;
@@ -223,7 +224,7 @@ extern "C" {
 tc_status tc_kvq_append(const tc_plan *plan, const tc_kvq_pool *pool, const void *k_new, const void *v_new, void *stream) {
     tc_status st = check_kvq(plan, pool);
     if (st != TC_OK || plan->T == 0) return st;
-    if ((st = check_kvq_rows(k_new, v_new)) != TC_OK || (st = check_kvq_device(plan)) != TC_OK) return st;
+    if ((st = check_kvq_rows(plan, k_new, v_new)) != TC_OK || (st = check_kvq_device(plan)) != TC_OK) return st;
     return device_result(tc::launch_kvq_append(plan, pool, k_new, v_new, stream), "tc_kvq_append launch");
 }
 
@@ -256,7 +257,7 @@ tc_status tc_kvq_mixed_attention_append(const tc_plan *plan, const tc_kvq_pool *
                                         void *out, float scale, void *workspace, size_t workspace_bytes, void *stream) {
     tc_status st = check_kvq(plan, pool);
     if (st != TC_OK || plan->T == 0) return st;
-    if ((st = check_kvq_rows(k_new, v_new)) != TC_OK) return st;
+    if ((st = check_kvq_rows(plan, k_new, v_new)) != TC_OK) return st;
     if ((st = check_kvq_attention(plan, q, out, scale, workspace, workspace_bytes)) != TC_OK || (st = check_kvq_device(plan)) != TC_OK) return st;
     const bool apart = tc::kvq_append_apart(plan);
     if (apart) {

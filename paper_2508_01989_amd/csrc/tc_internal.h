@@ -77,7 +77,7 @@ struct PlanScratch {
     std::vector<PlanRun> runs;
     std::vector<PlanTeam> teams;
     std::vector<int> wg_fill, open;
-    std::vector<int32_t> n_teams, slot0, merge_of;
+    std::vector<int32_t> n_teams, slot0, merge_of, seen;
     std::vector<PlanUnits> units;
 };
 
@@ -87,6 +87,7 @@ struct tc_plan {
     int Hq = 0, Hkv = 0, D = 0, G = 0;
     int dtype = TC_BF16;  // element type of q / k / v / out: selects the MFMA instantiation
     bool kvq = false;     // the pools hold 8 bits an element (TC_KV_E4M3): a plan is for one kind of pools
+    bool append_shared = false;  // of 8 bits: two of the append segments are for the same block
     int64_t num_blocks = 0;
     int S = 0, T = 0;
     int n_prefill_seqs = 0, n_decode_seqs = 0;

@@ -929,6 +929,20 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
             if (pass == 0) p->n_append_prefill = (int)((ap - (H + off_append)) / kAppendInts);
         }
     }
+    p->append_shared = false;
+    if (kvq) {  // (in 8 bits a segment's wave rewrites the whole block)
+        size_t size = 16;
+        int shift = 28;
+        while (size < 2 * (size_t)n_append) size *= 2, shift--;
+        w.seen.assign(size, -1);
+        for (int64_t i = 0; i < n_append && !p->append_shared; i++) {
+            const int32_t id = H[off_append + i * kAppendInts + 3];
+            size_t at = ((uint32_t)id * 2654435761u) >> shift;
+            while (w.seen[at] >= 0 && w.seen[at] != id) at = (at + 1) & (size - 1);
+            p->append_shared = w.seen[at] == id;
+            w.seen[at] = id;
+        }
+    }
 
     // ---- prefill items in `blocks` order with the KV head as the fastest index; the merge items and partial
     // slots of cut items; then pieces and workgroups.  Workgroup id mod Hkv names the KV head, so that with

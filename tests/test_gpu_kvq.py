@@ -86,7 +86,7 @@ class Case:
 
 
 class Device:
-    def __init__(self, tc, c, device="cuda:0", stream=None, poison=0x7F):
+    def __init__(self, tc, c, device="cuda:0", stream=None, poison=0x7F, one_by_one=False):
         import torch
         self.tc, self.c, self.torch = tc, c, torch
         self.stream = stream
@@ -97,10 +97,10 @@ class Device:
         self.pool = tc.make_kvq_pool(c.Hq, c.Hkv, c.D, c.blocks, self.k, self.v, self.scales, dtype=tc.TC_FP16 if c.dtype == "fp16" else tc.TC_BF16)
         self.q, self.k_new, self.v_new, kh, vh = (up(x) for x in (c.q, c.k_new, c.v_new, c.k_hist, c.v_hist))
         has = np.flatnonzero(c.ctx > 0)
-        if len(has):
-            start = np.concatenate([[0], np.cumsum(c.ctx[has])]).astype(np.int32)
-            plan = tc.Plan(self.pool, start, np.zeros(len(has), np.int32), c.table[has])
-            tc.tc_kvq_append(plan, self.pool, kh, vh)
+        for part in (has.reshape(-1, 1) if one_by_one else [has] if len(has) else []):
+            start = np.concatenate([[0], np.cumsum(c.ctx[part])]).astype(np.int32)
+            plan = tc.Plan(self.pool, start, np.zeros(len(part), np.int32), c.table[part])
+            tc.tc_kvq_append(plan, self.pool, kh[c.h_start[part[0]]:], vh[c.h_start[part[0]]:])
             torch.cuda.synchronize()
             plan.destroy()
         self.plan = tc.Plan(self.pool, c.q_start, c.ctx, c.table)
@@ -360,7 +360,7 @@ def test_sequences_that_share_their_first_blocks(tc):
             x[c.h_start[s]:c.h_start[s] + 96] = x[:96]
     print("[case] shared blocks", flush=True)
     cache = c.oracle_cache()
-    dev = Device(tc, c)
+    dev = Device(tc, c, one_by_one=True)  # (a call whose rows go to the same block twice is refused)
     dev.step()
     check_cache(dev, cache, "step")
     want, bound = c.attention(cache)

@@ -241,3 +241,23 @@ def test_empty_batch_and_too_many_tokens(tc):
     big = tc.Plan(pool, np.arange((1 << 10) + 1, dtype=np.int32), np.full(1 << 10, n - 1, np.int32), table, host_only=True)
     assert _status(tc, tc.tc_kvq_read, big, pool, -1, A, A) == tc.TC_ERR_ARG and "2^31" in tc.last_error()
     assert _status(tc, tc.tc_kvq_read, big, pool, 5, A, A) == tc.TC_ERR_ARG and "host-only" in tc.last_error()
+
+
+def test_two_sequences_that_append_to_the_same_block_are_refused(tc):
+    """Attention over what is there, and reading it, are not: both may end in a block that they share."""
+    pool = _pool(tc)
+    for q_len, ctx, rows in [((1, 1), (20, 25), ((3, 7), (9, 7))), ((40, 1), (0, 3), ((1, 2, 3), (2, 0, 0))), ((1, 1, 1), (0, 16, 31), ((5, 0), (6, 4), (6, 5))),
+                             ((17,), (0,), ((4, 4),))]:
+        table = np.zeros((len(rows), 3), np.int32)
+        for s, r in enumerate(rows):
+            table[s, :len(r)] = r
+        p = tc.Plan(pool, np.concatenate([[0], np.cumsum(q_len)]), np.array(ctx), table, host_only=True)
+        calls = _calls(tc, p, pool)
+        for name in ("append", "step"):
+            assert _status(tc, calls[name]) == tc.TC_ERR_BLOCK, (q_len, name)
+        for name in ("read", "attention"):
+            assert _status(tc, calls[name]) == tc.TC_ERR_ARG and "host-only" in tc.last_error(), (q_len, name)
+    # the shared blocks of a common prompt get no rows
+    p = tc.Plan(pool, np.array([0, 1, 3]), np.array([35, 34]), np.array([[1, 2, 3], [1, 2, 4]]), host_only=True)
+    for name, call in _calls(tc, p, pool).items():
+        assert _status(tc, call) == tc.TC_ERR_ARG and "host-only" in tc.last_error(), name
