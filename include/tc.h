@@ -116,6 +116,8 @@ typedef struct {
                                         /* decodes) or half of them                                                   */
     int64_t build_ns;                   /* host time of the latest work-list build ...       */
     int64_t upload_ns;                  /* ... and of enqueueing its copy to the device      */
+    int32_t append_launch;              /* 1: the call that appends and attends stores the new rows in a launch of    */
+                                        /* its own before the attention's                                             */
 } tc_plan_info;
 
 /* Validate the batch against the pool shape, build the work list and upload it on
@@ -257,9 +259,9 @@ typedef struct {
  * 448 * 2^e in magnitude, or the exponent the block had if that is larger and the sequence has earlier rows in the block.  A new
  * element x becomes the E4M3 number nearest to x * 2^-e (ties to even; where limited, the largest); infinities and NaN become
  * NaN.  Where e grows, the block's earlier rows are brought to it the same way, which changes only numbers below 2^-6 of the
- * new scale.  What a block holds beyond the sequence's last token is left as it was.  A block that gets rows must belong
- * to one sequence of the batch only (TC_ERR_BLOCK if two sequences would put rows into the same one); what the call leaves depends on the rows and the cache alone, and making it again changes
- * nothing. */
+ * new scale.  What a block holds beyond the sequence's last token is left as it was.  A block may get rows from one
+ * place of the batch's tables only (TC_ERR_BLOCK if two sequences, or two pages of one, would put rows into the same one); the others that hold it
+ * attend over what the append leaves.  What the call leaves depends on the rows and the cache alone, and making it again changes nothing. */
 tc_status tc_kvq_append(const tc_plan *plan, const tc_kvq_pool *pool, const void *k_new, const void *v_new, void *stream);
 
 /* Read a cache in 8 bits back: k_out, v_out DEVICE [n][Hkv][D] get what tokens 0..ctx+q_len-1 of sequence `seq`, or of all
@@ -273,7 +275,8 @@ tc_status tc_kvq_read(const tc_plan *plan, const tc_kvq_pool *pool, int32_t seq,
 tc_status tc_kvq_mixed_attention(const tc_plan *plan, const tc_kvq_pool *pool, const void *q, void *out, float scale,
                                  void *workspace, size_t workspace_bytes, void *stream);
 
-/* tc_kvq_append and tc_kvq_mixed_attention of the same batch in one call; cache and outputs are bit for bit those of the two. */
+/* tc_kvq_append and tc_kvq_mixed_attention of the same batch in one call; cache and outputs are bit for bit those of the two.  One launch, or two
+ * (tc_plan_info.append_launch): for chunks, long streams of decodes, and decodes of which one attends over a block that another's row goes into. */
 tc_status tc_kvq_mixed_attention_append(const tc_plan *plan, const tc_kvq_pool *pool, const void *q, const void *k_new,
                                         const void *v_new, void *out, float scale, void *workspace, size_t workspace_bytes,
                                         void *stream);

@@ -66,7 +66,7 @@ tc_status tc_mixed_attention_append(const tc_plan *plan, const tc_kv_pool *pool,
     // A batch with a prefill chunk: the chunk's rows are read by many workgroups of the attention kernel, which may not
     // wait for one another, so all rows are stored first, by the append kernel (the two calls in one).  A batch of
     // decodes: one launch, whose last workgroups store the rows while the grid drains.
-    if (plan->n_pieces > 0) {
+    if (plan->append_apart) {
         st = device_result(tc::launch_kv_append(plan, pool, k_new, v_new, false, stream), "tc_mixed_attention_append launch");
         if (st != TC_OK) return st;
     }
@@ -259,7 +259,7 @@ tc_status tc_kvq_mixed_attention_append(const tc_plan *plan, const tc_kvq_pool *
     if (st != TC_OK || plan->T == 0) return st;
     if ((st = check_kvq_rows(plan, k_new, v_new)) != TC_OK) return st;
     if ((st = check_kvq_attention(plan, q, out, scale, workspace, workspace_bytes)) != TC_OK || (st = check_kvq_device(plan)) != TC_OK) return st;
-    const bool apart = tc::kvq_append_apart(plan);
+    const bool apart = plan->append_apart;
     if (apart) {
         st = device_result(tc::launch_kvq_append(plan, pool, k_new, v_new, stream), "tc_kvq_mixed_attention_append launch");
         if (st != TC_OK) return st;

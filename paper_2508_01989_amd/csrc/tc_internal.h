@@ -77,7 +77,8 @@ struct PlanScratch {
     std::vector<PlanRun> runs;
     std::vector<PlanTeam> teams;
     std::vector<int> wg_fill, open;
-    std::vector<int32_t> n_teams, slot0, merge_of, seen;
+    std::vector<int32_t> n_teams, slot0, merge_of;
+    std::vector<uint64_t> gets_rows;  // a bit for each block of the pool, all zero between builds
     std::vector<PlanUnits> units;
 };
 
@@ -88,6 +89,7 @@ struct tc_plan {
     int dtype = TC_BF16;  // element type of q / k / v / out: selects the MFMA instantiation
     bool kvq = false;     // the pools hold 8 bits an element (TC_KV_E4M3): a plan is for one kind of pools
     bool append_shared = false;  // of 8 bits: two of the append segments are for the same block
+    bool append_apart = false;  // the call that appends and attends stores the rows in a launch of its own, before the attention
     int64_t num_blocks = 0;
     int S = 0, T = 0;
     int n_prefill_seqs = 0, n_decode_seqs = 0;
@@ -162,8 +164,6 @@ int launch_kv_migrate(const tc_plan *p, bool import, int page0, int n_pages, int
 // A cache in 8 bits (tc_kvq.hip).
 int launch_kvq_append(const tc_plan *p, const tc_kvq_pool *pool, const void *k_new, const void *v_new, void *stream);
 int launch_kvq_read(const tc_plan *p, const tc_kvq_pool *pool, int page0, int n_pages, void *k_out, void *v_out, void *stream);
-// Whether tc_kvq_mixed_attention_append stores the rows in a launch of its own, before the attention.
-bool kvq_append_apart(const tc_plan *p);
 // k_new / v_new non-null (not where the rows are stored apart): the kernel also stores the rows.
 int launch_kvq_attention(const tc_plan *p, const tc_kvq_pool *pool, const void *q, const void *k_new, const void *v_new, void *out, float scale, void *workspace,
                          void *stream);

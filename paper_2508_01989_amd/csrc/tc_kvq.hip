@@ -226,17 +226,6 @@ int launch_kvq_append(const tc_plan *p, const tc_kvq_pool *pool, const void *k_n
     return by_shape(p, [&](auto d, auto e) { return append_d<decltype(d)::value, decltype(e)>(p, pool, k_new, v_new, (hipStream_t)stream); });
 }
 
-// The rows of a chunk are read by many workgroups of the attention kernel, which may not wait for one another, so they are stored before it.  A batch of
-// decodes is one launch, whose waves with a sequence's last page store its row, unless single waves stream half a gigabyte and more: the waves' stores, of
-// 16-byte pieces into lines that nobody else touches, then cost the stream more than a launch of 5 us before it, which the host does not wait for.  Measured
-// (us per step, in one launch / two; 32/8 heads, head_dim 128, unless stated):
-//   400 MB   32/32 heads, 100 of mean 500 73.6 / 74.0            520   512 of mean 500 97.0 / 96.3, 40/8, head_dim 64, of 1000 92.1 / 91.1, but 16/2, of 2000 87.4 / 88.4
-//   800      512 of mean 800 148.6 / 143.8, 256 of 1500 133.6 / 131.8, 64/8, 300 of 1300 146.2 / 143.5      1000 128 of 4000 168.4 / 168.3, 40/8, head_dim 64, 512 of 2000 174.5 / 171.2
-//   2100     512 of 1000-3000 355.5 / 347.0                      small  400 of 20-60 13.3 / 16.0, 100 of them 6.6 / 9.1, head_dim 64, 64 of 1000-3000 22.8 / 26.0
-bool kvq_append_apart(const tc_plan *p) {
-    return p->n_pieces > 0 || (p->waves_per_item == 1 && p->total_pages * p->Hkv * (2 * kBlock * p->D) >= (int64_t)500000000);
-}
-
 int launch_kvq_read(const tc_plan *p, const tc_kvq_pool *pool, int page0, int n_pages, void *k_out, void *v_out, void *stream) {
     if (n_pages == 0) return 0;
     return by_shape(p, [&](auto d, auto e) { return read_d<decltype(d)::value, decltype(e)>(p, pool, page0, n_pages, k_out, v_out, (hipStream_t)stream); });

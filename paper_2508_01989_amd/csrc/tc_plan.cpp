@@ -521,6 +521,20 @@ static int64_t deal_units(const tc_plan *p, int n_wg_head, bool level_runs, int6
     return dealt;
 }
 
+// Whether the call that appends and attends stores the rows in a launch of its own.
+// The rows of a chunk are read by many workgroups of the attention kernel, which may not wait for one another, so they are stored before it.  A batch of
+// decodes is one launch, whose waves with a sequence's last page store its row (in 16 bits: or workgroups at the end of the grid), unless a block that gets rows
+// stands in another place of the tables (see build_plan), where a wave that attends over it would read its exponents and bytes while they are rewritten.
+// In 8 bits, too, where single waves stream half a gigabyte and more: the waves' stores, of 16-byte pieces into lines that nobody else touches, then cost
+// the stream about as much as a launch of 5 us before it, which the host does not wait for, or more.  Measured (us per step, in one launch / two; 32/8 heads, head_dim 128, unless stated):
+//   400 MB   32/32 heads, 100 of mean 500 73.6 / 74.0            520   512 of mean 500 97.0 / 96.3, 40/8, head_dim 64, of 1000 92.1 / 91.1, but 16/2, of 2000 87.4 / 88.4
+//   800      512 of mean 800 148.6 / 143.8, 256 of 1500 133.6 / 131.8, 64/8, 300 of 1300 146.2 / 143.5      1000 128 of 4000 168.4 / 168.3, 40/8, head_dim 64, 512 of 2000 174.5 / 171.2
+//   2100     512 of 1000-3000 355.5 / 347.0                      small  400 of 20-60 13.3 / 16.0, 100 of them 6.6 / 9.1, head_dim 64, 64 of 1000-3000 22.8 / 26.0
+// (between 400 and 1000 MB the two are within a few per cent of each other on either side of the line)
+static bool append_apart_by_size(const tc_plan *p, bool chunks, int64_t pages) {
+    return chunks || (p->kvq && p->waves_per_item == 1 && pages * p->Hkv * (2 * kBlock * p->D) >= (int64_t)500000000);
+}
+
 tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     if (!p || !pool || !b) return fail(TC_ERR_NULL, "plan, pool or batch is NULL");
     // an error below leaves the plan describing an empty batch
@@ -528,6 +542,7 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     p->n_prefill_seqs = p->n_decode_seqs = 0;
     p->n_prefill = p->n_decode = p->n_merge = p->n_partials = p->n_piece_partials = p->n_merge_prefill = p->n_pieces = p->n_prefill_wg = p->n_counters = p->n_append = p->n_append_prefill = p->n_decode_wg = p->n_dealt = p->n_drawers = 0;
     p->queue_counter = -1;
+    p->append_shared = p->append_apart = false;
     p->items_per_wg = kDecodeWaves;
     p->waves_per_item = 1;
     p->rows_per_item = kPrefillRows;
@@ -929,19 +944,24 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
             if (pass == 0) p->n_append_prefill = (int)((ap - (H + off_append)) / kAppendInts);
         }
     }
-    p->append_shared = false;
-    if (kvq) {  // (in 8 bits a segment's wave rewrites the whole block)
-        size_t size = 16;
-        int shift = 28;
-        while (size < 2 * (size_t)n_append) size *= 2, shift--;
-        w.seen.assign(size, -1);
-        for (int64_t i = 0; i < n_append && !p->append_shared; i++) {
+    // Blocks that get rows: from two places of the tables (in 8 bits a segment's wave rewrites the whole block, so the appends refuse that), and such that stand in
+    // another place too, whose attention must not run beside the append.  A sum over all pages, 0.4 ns each, so only where it decides.
+    p->append_apart = append_apart_by_size(p, !w.pieces.empty(), pages);
+    if (kvq) {
+        if (w.gets_rows.size() * 64 < (size_t)p->num_blocks) w.gets_rows.resize(((size_t)p->num_blocks + 63) / 64, 0);
+        const auto word = [&](int32_t id) -> uint64_t & { return w.gets_rows[id >> 6]; };
+        int64_t blocks = 0, places = 0;
+        for (int64_t i = 0; i < n_append; i++) {
             const int32_t id = H[off_append + i * kAppendInts + 3];
-            size_t at = ((uint32_t)id * 2654435761u) >> shift;
-            while (w.seen[at] >= 0 && w.seen[at] != id) at = (at + 1) & (size - 1);
-            p->append_shared = w.seen[at] == id;
-            w.seen[at] = id;
+            blocks += !(word(id) >> (id & 63) & 1);
+            word(id) |= (uint64_t)1 << (id & 63);
         }
+        p->append_shared = blocks < n_append;
+        if (!p->append_apart) {
+            for (int64_t i = 0; i < pages; i++) places += word(H[off_pages + i]) >> (H[off_pages + i] & 63) & 1;
+            p->append_apart = places > blocks;
+        }
+        for (int64_t i = 0; i < n_append; i++) word(H[off_append + i * kAppendInts + 3]) = 0;
     }
 
     // ---- prefill items in `blocks` order with the KV head as the fastest index; the merge items and partial
@@ -1119,6 +1139,7 @@ tc_status tc_plan_get_info(const tc_plan *p, tc_plan_info *info) {
     info->num_prefill_workgroups = p->n_prefill_wg;
     info->num_counters = p->n_counters;
     info->decode_queue = p->n_drawers > p->n_decode_wg;  // the prefill workgroups draw too
+    info->append_launch = p->append_apart;
     info->build_ns = p->build_ns;
     info->upload_ns = p->upload_ns;
     return TC_OK;

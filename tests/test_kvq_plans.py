@@ -1,0 +1,57 @@
+"""The KV cache in 8 bits on the CPU: what plans say about batches whose tables share blocks, and the forms that chunks take."""
+import numpy as np
+import pytest
+
+from test_abi_host import tc  # noqa: F401  (the fixture)
+
+
+def plan(tc, ctx, rows, q_len=None, Hq=8, Hkv=2, D=128, nb=4000, **kw):
+    q_len = q_len or [1] * len(ctx)
+    table = np.zeros((len(rows), max(len(r) for r in rows)), np.int32)
+    for s, r in enumerate(rows):
+        table[s, :len(r)] = r
+    q_start = np.concatenate([[0], np.cumsum(q_len)]).astype(np.int32)
+    return tc.Plan(tc.make_kvq_pool(Hq, Hkv, D, nb, **kw), q_start, np.array(ctx, np.int32), table, host_only=True)
+
+
+def test_decodes_that_attend_over_a_block_which_gets_rows_have_their_append_apart(tc):
+    """Two rows of one request on either side of a page boundary: the second attends over the block that the first's row goes into (and may change the
+    scale of), so both may not happen in one launch."""
+    many = [[100 + 8 * i + j for j in range(8)] for i in range(400)]
+    ctx = [100 + i % 20 for i in range(400)]
+    for name, apart, p in [
+            ("no block in two places", 0, plan(tc, [15, 16], [[3], [4, 5]])),
+            ("a common prompt", 0, plan(tc, [32, 40, 47], [[1, 2, 3], [1, 2, 4], [1, 2, 5]])),
+            ("either side of a boundary", 1, plan(tc, [15, 16], [[3], [3, 5]])),
+            ("in the other order", 1, plan(tc, [16, 15], [[3, 5], [3]])),
+            ("far from the end", 1, plan(tc, [3, 3000], [[7], list(range(20, 200)) + [7] + list(range(200, 207))])),
+            ("twice in its own table", 1, plan(tc, [31], [[6, 6]])),
+            ("beside a common prompt", 1, plan(tc, [32, 63, 64], [[1, 2, 3], [1, 2, 4, 5], [1, 2, 4, 5, 6]])),
+            ("single waves", 0, plan(tc, ctx, many)),
+            ("single waves, one of them", 1, plan(tc, ctx[:399] + [100], many[:399] + [many[5][:6] + [many[5][6]]])),
+            ("ids whose last bits are alike", 0, plan(tc, [15, 16], [[3], [3 + (1 << 15), 3 + (1 << 16)]], nb=1 << 17)),
+            ("the entries beyond the last token do not count", 0, plan(tc, [15, 16], [[3, 5], [4, 5]]))]:
+        assert p.info.append_launch == apart, name
+    # a batch with a chunk stores its rows first in any case
+    assert plan(tc, [0, 3], [[1, 2], [3]], q_len=[20, 1]).info.append_launch == 1
+
+
+def test_an_update_forgets_the_blocks_of_the_batch_before(tc):
+    p = plan(tc, [15, 16], [[3], [3, 5]])
+    assert p.info.append_launch == 1
+    pool = tc.make_kvq_pool(8, 2, 128, 4000)
+    p.update(pool, np.array([0, 1, 2], np.int32), np.array([15, 16], np.int32), np.array([[3, 0], [4, 5]], np.int32))
+    assert p.info.append_launch == 0
+
+
+@pytest.mark.parametrize("seed", range(20))
+def test_tables_of_random_batches(tc, seed):
+    rng = np.random.default_rng(seed)
+    n = int(rng.integers(1, 30))
+    ctx = rng.integers(0, 400, n)
+    pages = ctx // 16 + 1
+    nb = int(rng.integers(4, 30)) * int(pages.sum())
+    rows = [rng.integers(0, nb, k).tolist() for k in pages]
+    ids, last = np.concatenate(rows), [r[-1] for r in rows]
+    p = plan(tc, ctx, rows, nb=nb)
+    assert p.info.append_launch == int(len(set(last)) < sum(int((ids == b).sum()) for b in set(last)))
