@@ -198,7 +198,8 @@ tc_status tc_mixed_attention(const tc_plan *plan, const tc_kv_pool *pool, const 
                              void *workspace, size_t workspace_bytes, void *stream);
 
 /* tc_kv_append and tc_mixed_attention of the same batch in one call (paper Sec. 2.1: the new tokens'
- * K and V are cached as part of the iteration that computes them).  A batch of decodes is ONE launch:
+ * K and V are cached as part of the iteration that computes them).  A batch of decodes is ONE launch, unless one of them attends over a block that another's
+ * row goes into (tc_plan_info.append_launch):
  * the wavefront that runs a sequence's last KV split takes the new token's K and V from k_new / v_new
  * (they replace, in registers, what the page fetch found in that slot), and the last workgroups of the
  * same launch store the rows into the pool; nobody waits for anybody.  The rows of a prefill chunk are

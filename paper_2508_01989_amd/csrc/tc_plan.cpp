@@ -524,7 +524,8 @@ static int64_t deal_units(const tc_plan *p, int n_wg_head, bool level_runs, int6
 // Whether the call that appends and attends stores the rows in a launch of its own.
 // The rows of a chunk are read by many workgroups of the attention kernel, which may not wait for one another, so they are stored before it.  A batch of
 // decodes is one launch, whose waves with a sequence's last page store its row (in 16 bits: or workgroups at the end of the grid), unless a block that gets rows
-// stands in another place of the tables (see build_plan), where a wave that attends over it would read its exponents and bytes while they are rewritten.
+// stands in another place of the tables (see build_plan): a wave that attends over it there would find the new row or not (in 8 bits read exponents and bytes
+// while they are rewritten).
 // In 8 bits, too, where single waves stream half a gigabyte and more: the waves' stores, of 16-byte pieces into lines that nobody else touches, then cost
 // the stream about as much as a launch of 5 us before it, which the host does not wait for, or more.  Measured (us per step, in one launch / two; 32/8 heads, head_dim 128, unless stated):
 //   400 MB   32/32 heads, 100 of mean 500 73.6 / 74.0            520   512 of mean 500 97.0 / 96.3, 40/8, head_dim 64, of 1000 92.1 / 91.1, but 16/2, of 2000 87.4 / 88.4
@@ -945,9 +946,9 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
         }
     }
     // Blocks that get rows: from two places of the tables (in 8 bits a segment's wave rewrites the whole block, so the appends refuse that), and such that stand in
-    // another place too, whose attention must not run beside the append.  A sum over all pages, 0.4 ns each, so only where it decides.
+    // another place too, whose attention must not run beside the append.  A sum over all pages, half a nanosecond each, so only where it decides.
     p->append_apart = append_apart_by_size(p, !w.pieces.empty(), pages);
-    if (kvq) {
+    if (kvq || !p->append_apart) {
         if (w.gets_rows.size() * 64 < (size_t)p->num_blocks) w.gets_rows.resize(((size_t)p->num_blocks + 63) / 64, 0);
         const auto word = [&](int32_t id) -> uint64_t & { return w.gets_rows[id >> 6]; };
         int64_t blocks = 0, places = 0;
@@ -956,9 +957,14 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
             blocks += !(word(id) >> (id & 63) & 1);
             word(id) |= (uint64_t)1 << (id & 63);
         }
-        p->append_shared = blocks < n_append;
+        p->append_shared = kvq && blocks < n_append;
         if (!p->append_apart) {
-            for (int64_t i = 0; i < pages; i++) places += word(H[off_pages + i]) >> (H[off_pages + i] & 63) & 1;
+            const uint64_t *bits = w.gets_rows.data();
+            for (int s = 0; s < S; s++) {
+                const int32_t *row = b->block_table + (int64_t)s * b->max_blocks;
+                const int np = p->page_off[s + 1] - p->page_off[s];
+                for (int i = 0; i < np; i++) places += bits[row[i] >> 6] >> (row[i] & 63) & 1;
+            }
             p->append_apart = places > blocks;
         }
         for (int64_t i = 0; i < n_append; i++) word(H[off_append + i * kAppendInts + 3]) = 0;

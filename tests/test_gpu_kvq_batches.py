@@ -1,10 +1,12 @@
-"""The KV cache in 8 bits on the GPU: batches whose sequences share blocks, special numbers in every form.  Cases, oracle and bounds are those of test_gpu_kvq.py."""
+"""Batches on the GPU whose sequences share blocks that get rows, and special numbers in every form of the 8-bit cache.  Cases, oracle and bounds are those of test_gpu_kvq.py."""
 import copy
 
 import numpy as np
 import pytest
 
-from test_gpu_kvq import Case, Device, bits_of, check_attention, check_cache, tc  # noqa: F401  (tc: the fixture)
+import oracle
+from oracle import kvq
+from test_gpu_kvq import HALF_STEP, Case, Device, bits_of, check_attention, check_cache, tc  # noqa: F401  (tc: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +46,50 @@ def test_decodes_that_attend_over_a_block_which_gets_rows(tc, R, Hq, Hkv, dtype)
         one.step()
         check_cache(one, cache, "step")
         assert np.array_equal(one.outputs(), two.outputs())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("R,Hq,Hkv", [(3, 8, 2), (120, 32, 8)])  # a split is run by a workgroup, by a wave
+def test_decodes_that_attend_over_a_block_which_gets_rows_in_16_bits(tc, R, Hq, Hkv, dtype):
+    """The same batches, and pairs in one block, over a cache in 16 bits: one call gives the bits of the two, and those of the plain form's pools."""
+    import torch
+    c = both_sides_of_a_boundary(R, Hq, Hkv, 64, dtype)
+    ctx = c.ctx.copy()
+    for i in range(0, R, 2):  # every other pair one position sooner: both rows in the same block
+        ctx[2 * i:2 * i + 2] -= 1
+    kv = ctx + 1
+    up = lambda a: torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).to("cuda:0")  # noqa: E731
+    n, code = c.blocks * Hkv * 16 * 64, tc.TC_FP16 if dtype == "fp16" else tc.TC_BF16
+    k0, v0 = oracle.new_pool(c.blocks, Hkv, 64)
+    for s in range(c.S):
+        a = c.h_start[s]
+        oracle.kv_append(k0, v0, Hkv, 64, 16, np.array([0, ctx[s]], np.int32), np.zeros(1, np.int32), c.table[s:s + 1], c.k_hist[a:a + ctx[s]], c.v_hist[a:a + ctx[s]])
+    q, k_new, v_new, got = up(c.q), up(c.k_new), up(c.v_new), []
+    print(f"[case] boundary, 16 bits, {R} {dtype}", flush=True)
+    for both in (False, True, True):
+        k, v = up(k0), up(v0)
+        assert k.numel() == n
+        pool = tc.make_pool(Hq, Hkv, 64, c.blocks, k, v, dtype=code)
+        plan = tc.Plan(pool, c.q_start, ctx, c.table)
+        assert plan.info.append_launch == 1 and (plan.info.waves_per_item == 1) == (R == 120)
+        ws = torch.empty(max(16, plan.workspace_bytes), dtype=torch.uint8, device="cuda:0")
+        out = torch.zeros((c.S, Hq, 64), dtype=torch.int16, device="cuda:0")
+        if both:
+            tc.tc_mixed_attention_append(plan, pool, q, k_new, v_new, out, c.scale, ws)
+        else:
+            tc.tc_kv_append(plan, pool, k_new, v_new)
+            tc.tc_mixed_attention(plan, pool, q, out, c.scale, ws)
+        torch.cuda.synchronize()
+        got.append((k, v, out))
+    for x in got[1:]:
+        for y, z in zip(got[0], x):
+            assert torch.equal(y, z)
+    oracle.kv_append(k0, v0, Hkv, 64, 16, c.q_start, ctx, c.table, c.k_new, c.v_new)
+    assert np.array_equal(got[0][0].cpu().numpy().view(np.uint16).reshape(k0.shape), k0) and np.array_equal(got[0][1].cpu().numpy().view(np.uint16).reshape(v0.shape), v0)
+    args = (Hq, Hkv, 64, 16, c.q_start, ctx, c.table, c.q, c.scale)
+    otype = oracle.FP16 if dtype == "fp16" else oracle.BF16
+    want, mean = oracle.attention(k0, v0, *args, dtype=otype), oracle.attention(k0, v0 & np.uint16(0x7FFF), *args, dtype=otype)
+    bound = HALF_STEP[dtype] * 1.02 * (mean + np.abs(want)) + 1e-30
+    if dtype == "fp16":  # (small probabilities, see test_gpu_kvq.py)
+        bound += int(kv.max()) * 2.0 ** -25 * max(float(np.abs(kvq.widen(x, "fp16")).max()) for x in (c.v_new, c.v_hist))
+    check_attention(kvq.widen(got[0][2].cpu().numpy().view(np.uint16), dtype), want, bound, "16 bits")

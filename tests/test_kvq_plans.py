@@ -1,17 +1,20 @@
-"""The KV cache in 8 bits on the CPU: what plans say about batches whose tables share blocks, and the forms that chunks take."""
+"""Plans on the CPU: what they say about batches whose tables share blocks, in 8 and in 16 bits, and the forms that chunks take in 8 bits."""
 import numpy as np
 import pytest
 
 from test_abi_host import tc  # noqa: F401  (the fixture)
 
 
-def plan(tc, ctx, rows, q_len=None, Hq=8, Hkv=2, D=128, nb=4000, **kw):
+BITS = {8: "make_kvq_pool", 16: "make_pool"}
+
+
+def plan(tc, ctx, rows, q_len=None, Hq=8, Hkv=2, D=128, nb=4000, bits=8):
     q_len = q_len or [1] * len(ctx)
     table = np.zeros((len(rows), max(len(r) for r in rows)), np.int32)
     for s, r in enumerate(rows):
         table[s, :len(r)] = r
     q_start = np.concatenate([[0], np.cumsum(q_len)]).astype(np.int32)
-    return tc.Plan(tc.make_kvq_pool(Hq, Hkv, D, nb, **kw), q_start, np.array(ctx, np.int32), table, host_only=True)
+    return tc.Plan(getattr(tc, BITS[bits])(Hq, Hkv, D, nb), q_start, np.array(ctx, np.int32), table, host_only=True)
 
 
 def test_decodes_that_attend_over_a_block_which_gets_rows_have_their_append_apart(tc):
@@ -55,3 +58,15 @@ def test_tables_of_random_batches(tc, seed):
     ids, last = np.concatenate(rows), [r[-1] for r in rows]
     p = plan(tc, ctx, rows, nb=nb)
     assert p.info.append_launch == int(len(set(last)) < sum(int((ids == b).sum()) for b in set(last)))
+
+
+def test_decodes_in_16_bits_that_attend_over_a_block_which_gets_rows(tc):
+    """The same: what the second would find in the first's slot depends on which of them is sooner."""
+    for apart, ctx, rows in [(0, [15, 16], [[3], [4, 5]]), (0, [32, 40], [[1, 2, 3], [1, 2, 4]]), (1, [15, 16], [[3], [3, 5]]), (1, [3, 4], [[3], [3]]),
+                             (1, [40, 41, 2], [[1, 2, 3], [1, 2, 3], [9]]), (1, [31], [[6, 6]])]:
+        assert plan(tc, ctx, rows, bits=16).info.append_launch == apart, rows
+    many = [[100 + 8 * i + j for j in range(8)] for i in range(400)]
+    ctx = [100 + i % 20 for i in range(400)]
+    assert plan(tc, ctx, many, bits=16).info.append_launch == 0
+    assert plan(tc, ctx[:399] + [101], many[:399] + [many[0][:7]], bits=16).info.append_launch == 1
+    assert plan(tc, [0, 3], [[1, 2], [3]], q_len=[20, 1], bits=16).info.append_launch == 1
