@@ -324,6 +324,28 @@ static int64_t fitting_regions(const tc_plan *p, int S) {
     return std::max<int64_t>(0, (int64_t)kStaticScratchBytes - partials * p->G * row_bytes) / (kPrefillRows * row_bytes);
 }
 
+constexpr int kUncutTiles = 16;  // of the longest sweep: up to here the rows of an item are chosen for sweeps that are not cut
+
+// In 8 bits a unit runs one workgroup at a time, of items of 128 rows too.  Where those of first chunks are more than the units (257 to 384), some units run two, one after the other:
+// with the longest first, the unit of the m-th last of the first round gets the m-th of the second.  That is taken where it ends sooner than the longest whole item.
+// Measured (us, 256 rows / 128; 40/8 heads, head_dim 128): sixteen of 51 9.5 / 11.7, each at 300 17.2 / 21.7, eight of 102 11.3 / 12.9, five of 153 12.6 / 13.0, 24/8, sixteen of
+// 85 11.3 / 12.9; 816 26.3 / 19.4, at 200 30.9 / 22.2, 405 and 400 18.2 / 14.1; 104/8, 304 15.3 / 12.7; head_dim 64 alike (sixteen of 51 6.4 / 8.4, 816 18.6 / 13.8).
+static bool second_round_takes_longer(const tc_plan *p, int S, int tiles) {
+    const int pos = kPrefillRows / 2 / p->G;
+    int64_t count[kUncutTiles + 1] = {};  // items by their tiles
+    for (int s = 0; s < S; s++) {
+        const int q = p->q_start[s + 1] - p->q_start[s];
+        for (int pos0 = 0; q > 1 && pos0 < q; pos0 += pos) count[(p->ctx_len[s] + std::min(pos0 + pos, q) - 1) / kPrefillTileTokens + 1] += p->Hkv;
+    }
+    int item[2 * kNumCu], n = 0;  // tiles of each, the longest first
+    for (int t = tiles; t > 0; t--)
+        for (int64_t i = 0; i < count[t] && n < 2 * kNumCu; i++) item[n++] = t;
+    const double half_us = p->D == 64 ? 0.62 : 1.1, whole_us = p->D == 64 ? 1.04 : 1.6, start = p->D == 64 ? 3.5 : 5.5;
+    double t_half = tiles * half_us + start;
+    for (int i = kNumCu; i < n; i++) t_half = std::max(t_half, (item[i] + item[2 * kNumCu - 1 - i]) * half_us + 2 * start);
+    return t_half > tiles * whole_us + start;
+}
+
 // Rows of a prefill item: 256, or 128 when the chunk is small.  An item of 128 rows keeps one wave per SIMD busy, and such a
 // wave sweeps a tile in about 0.6 of the time it takes beside a second one; but there are at least twice as many items,
 // by 128 / G against 256 / G positions more than twice where 256 / G is odd, three times for chunks of a few positions more than
@@ -368,10 +390,10 @@ static int choose_rows_per_item(const tc_plan *p, int S, int64_t decode_bytes) {
     if ((double)decode_bytes / 5.0e6 > tiles * kTileUs * (p->D / 128.0)) return kPrefillRows;
     int k_whole = 1, k_half = 1;
     double add_whole = 0;  // what starting and combining the longest pieces takes longer with 256 rows
-    const bool d64 = p->D == 64, cut = tiles > 16;
+    const bool d64 = p->D == 64, cut = tiles > kUncutTiles;
     if (!cut) {
         if (whole * 2 > kNumCu) return kPrefillRows;
-        if (decode_bytes == 0) return kPrefillRows / 2;
+        if (decode_bytes == 0) return p->kvq && half > kNumCu && second_round_takes_longer(p, S, tiles) ? kPrefillRows : kPrefillRows / 2;
     } else {
         if (whole * 8 > kNumCu || half > kNumCu) return kPrefillRows;
         k_whole = prefill_cuts(tiles, whole, decode_bytes, kCutTileUs);

@@ -70,3 +70,25 @@ def test_decodes_in_16_bits_that_attend_over_a_block_which_gets_rows(tc):
     assert plan(tc, ctx, many, bits=16).info.append_launch == 0
     assert plan(tc, ctx[:399] + [101], many[:399] + [many[0][:7]], bits=16).info.append_launch == 1
     assert plan(tc, [0, 3], [[1, 2], [3]], q_len=[20, 1], bits=16).info.append_launch == 1
+
+
+def chunk_form(tc, Hq, Hkv, chunks, decodes=(), D=128, bits=8):
+    """chunks: (tokens, offset); decodes: contexts"""
+    q_len, ctx = [n for n, _ in chunks] + [1] * len(decodes), [c for _, c in chunks] + list(decodes)
+    pages = [-(-(n + c) // 16) for n, c in zip(q_len, ctx)]
+    start = np.concatenate([[0], np.cumsum(pages)])
+    return plan(tc, ctx, [list(range(a, b)) for a, b in zip(start, start[1:])], q_len, Hq, Hkv, D, int(start[-1]) + 1, bits).info
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_first_chunks_whose_halves_would_take_two_rounds(tc, D):
+    """Items of 128 rows that are more than the compute units run one after the other in 8 bits: items of 256 where they are alike, halves where the
+    second round is of short ones."""
+    for Hq, Hkv, chunks, rows, items in [(40, 8, [(51, 0)] * 16, 256, 128), (40, 8, [(51, 300)] * 16, 256, 128), (40, 8, [(102, 0)] * 8, 256, 128),
+                                         (24, 8, [(85, 0)] * 16, 256, 128), (10, 2, [(51, 0)] * 64, 256, 128), (40, 8, [(816, 0)], 128, 264),
+                                         (40, 8, [(405, 0), (400, 0)], 128, 264), (104, 8, [(304, 0)], 128, 272), (40, 8, [(800, 0)], 128, 256)]:
+        i = chunk_form(tc, Hq, Hkv, chunks, D=D)
+        assert (i.rows_per_prefill_item, i.num_prefill_items, i.block_threads) == (rows, items, 512), chunks[:2]
+    # in 16 bits halves of four waves, several to a unit
+    i = chunk_form(tc, 40, 8, [(51, 0)] * 16, D=D, bits=16)
+    assert (i.rows_per_prefill_item, i.num_prefill_items, i.block_threads) == (128, 384, 256)
