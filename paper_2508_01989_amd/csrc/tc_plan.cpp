@@ -685,8 +685,8 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
             // Small workgroups: beside more decodes the queue fills the units whose sweeps end early; long sweeps run at a lower clock in either
             // form than the estimates say (6562 at 16848, 8/8 heads, 526 / 543).
             const double small_below = (w.blocks[0].n_tiles <= 64 ? 0.97 : 0.9) * t_whole;
-            if (kvq) t.small = 1e30;  // (the tiles of small workgroups in 16 bits and the pages in 8 do not fit the LDS of a unit)
-            bool small = t.small < small_below && t_decode < 0.05 * t.small;
+            const bool small_exists = !kvq;  // (in 8 bits the sweep has three stages of both tensors and two of the pages as they lie in the pool: one workgroup to a unit)
+            bool small = small_exists && t.small < small_below && t_decode < 0.05 * t.small;
             // That is by a unit's share of all sweeps.  Where some units have two long ones it is theirs that count, a tile of the fullest unit 0.9 us, 0.5 at
             // head_dim 64; for sweeps of up to 24 tiles it makes no difference.  (whole / small:) 16/2 heads, 2652 at 11274 and 2355 at 0 with 5
             // decodes 308 / 359, 64/8, 667 at 1657 and 356 at 0 62.4 / 69.3, head_dim 64, 685 at 12873 and 830 at 0 with 2 decodes 190 / 220.  Of 440 batches
@@ -709,12 +709,16 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
             // none (32/32 heads, 1136 at 174 with one of 1000 40.9 / 47.2, 776 at 1489 with 2 of 442-3540 58.5 / 63.1).  Instead of crowded small ones up to
             // three quarters of the units (40/8 heads, head_dim 64, 1204 at 4097 whole 82, runs 75); beyond whole items do as well or better (8/8, first
             // chunks of 2837, 3049 and 3264 92 / 108, 16/2, 4014 and 1489 95 / 103).
+            // In 8 bits, where there is nothing for them to be instead of, runs pay with fewer of them too: of 60 batches of 16 to 40 KV heads that have them only because of that,
+            // levelled 10 % faster on the mean, up to 40, the worst 10 % slower (whole / levelled: 32/32, 776 at 1489 with 2 of 442-3540 59.8 / 47.1, 1136 at 174 with one of 1000
+            // 36.6 / 37.1, 1240 at 0 and 41 at 4 36.6 / 29.0, 1044 at 805 with 7 of 209-836 51.0 / 44.5; 40/40, 792 at 2628 84.5 / 70.8, 967 at 68 32.2 / 35.5; head_dim 64, 32/32, 825 at
+            // 1321 with 2 39.8 / 30.5); of 60 that have them although they are fewer than eight a head, 22 %.
             const bool instead_of_small = !small && bins >= 8 && (!crowded || items * 4 <= 3 * kNumCu);
             // Every KV head has a unit at least: with more heads than units there is one run a head, which cuts nothing, more of them than run at once, and the queue
             // is for launches that all run from the start (us, runs / as they are: 257/257 heads, 200 at 4000 with 2 decodes 219 / 207; head_dim 64, 300/300, 69
             // at 8000 with 3 193 / 186, 320/320, 106 at 0 and 19 at 13305 with one 301 / 211, 514/257, 138 at 21684 with 2 1095 / 789).
             int runs = 0;
-            if (Hkv <= kNumCu && t_levelled < level_below * t_whole && (t_levelled < t.small || instead_of_small) && t_decode < 0.75 * t_levelled) {
+            if (Hkv <= kNumCu && t_levelled < level_below * t_whole && (!small_exists || t_levelled < t.small || instead_of_small) && t_decode < 0.75 * t_levelled) {
                 // (Chunks of up to three quarters of the units beside few decodes run like this whatever scratch they need.)
                 const bool any_scratch = items * 4 <= 3 * kNumCu && t_decode < 0.25 * w.blocks[0].n_tiles * kTileUs * (D / 128.0);
                 runs = level(bins, any_scratch);

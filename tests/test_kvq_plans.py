@@ -92,3 +92,12 @@ def test_first_chunks_whose_halves_would_take_two_rounds(tc, D):
     # in 16 bits halves of four waves, several to a unit
     i = chunk_form(tc, 40, 8, [(51, 0)] * 16, D=D, bits=16)
     assert (i.rows_per_prefill_item, i.num_prefill_items, i.block_threads) == (128, 384, 256)
+
+
+def test_chunks_of_few_runs_a_head_are_levelled_in_8_bits(tc):
+    """32 KV heads leave seven runs a head beside decodes: too few in 16 bits, where the same batches run whole."""
+    for chunk, decodes in [((1136, 174), [999]), ((776, 1489), [441, 3539])]:
+        i = chunk_form(tc, 32, 32, [chunk], decodes)
+        assert (i.num_prefill_workgroups, i.block_threads) == (7 * 32, 512) and i.num_piece_partials > 0 and i.num_prefill_pieces > i.num_prefill_items
+        i = chunk_form(tc, 32, 32, [chunk], decodes, bits=16)
+        assert i.num_prefill_workgroups == i.num_prefill_pieces == i.num_prefill_items and i.num_piece_partials == 0
