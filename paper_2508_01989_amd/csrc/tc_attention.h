@@ -1777,6 +1777,7 @@ __device__ __forceinline__ void decode_item_wide(const AttnArgs &A, const int32_
 // Tracing build (python -m paper_2508_01989_amd.build --trace): every workgroup of the attention kernel leaves the time
 // it started, the time its prefill pieces were done and the time it ended (100 MHz counter), and where it ran.
 constexpr int kTraceWorkgroups = 16384;
+// Each file of kernels has stamps of its own (a device variable belongs to its file), and a call that reads them.
 static __device__ long long g_wg_trace[kTraceWorkgroups * 4];
 __device__ __forceinline__ void wg_trace(long long t_start, long long t_mid, bool is_decode) {
     __syncthreads();

@@ -332,7 +332,7 @@ int static_scratch(int device, void **ptr, size_t *bytes) {
 }  // namespace tc
 
 #ifdef TC_WG_TRACE
-// Tracing build only: copy the first n int64 of the workgroup trace of the latest attention launch to HOST memory.
+// Tracing build only: copy the first n int64 of the workgroup trace of the latest attention launch (over a cache in 16 bits) to HOST memory.
 extern "C" int tc_debug_wg_trace(long long *dst, int n) {
     (void)hipDeviceSynchronize();
     return (int)hipMemcpyFromSymbol(dst, HIP_SYMBOL(tc::g_wg_trace), (size_t)n * sizeof(long long));

@@ -238,3 +238,11 @@ int launch_kvq_attention(const tc_plan *p, const tc_kvq_pool *pool, const void *
 }
 
 }  // namespace tc
+
+#ifdef TC_WG_TRACE
+// Tracing build only: tc_debug_wg_trace for launches over a cache in 8 bits.
+extern "C" int tc_debug_kvq_wg_trace(long long *dst, int n) {
+    (void)hipDeviceSynchronize();
+    return (int)hipMemcpyFromSymbol(dst, HIP_SYMBOL(tc::g_wg_trace), (size_t)n * sizeof(long long));
+}
+#endif
