@@ -6,7 +6,7 @@ import pytest
 
 import oracle
 from oracle import kvq
-from test_gpu_kvq import HALF_STEP, Case, Device, bits_of, check_attention, check_cache, tc  # noqa: F401  (tc: the fixture)
+from test_gpu_kvq import HALF_STEP, SPECIAL, Case, Device, bits_of, check_attention, check_cache, tc  # noqa: F401  (tc: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -93,3 +93,91 @@ def test_decodes_that_attend_over_a_block_which_gets_rows_in_16_bits(tc, R, Hq, 
     if dtype == "fp16":  # (small probabilities, see test_gpu_kvq.py)
         bound += int(kv.max()) * 2.0 ** -25 * max(float(np.abs(kvq.widen(x, "fp16")).max()) for x in (c.v_new, c.v_hist))
     check_attention(kvq.widen(got[0][2].cpu().numpy().view(np.uint16), dtype), want, bound, "16 bits")
+
+
+def attention_where_finite(c, cache):
+    """Case.attention with the bound's largest value taken from the finite ones."""
+    plain = copy.copy(c)
+    plain.v_new, plain.v_hist = (np.where(np.isfinite(kvq.widen(x, c.dtype)), x, 0).astype(np.uint16) for x in (c.v_new, c.v_hist))
+    return plain.attention(cache)  # (the cache holds what the tokens stand for: outputs are those of the batch itself)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("name", SPECIAL)
+def test_rows_beside_nan_are_within_the_bound(tc, name, dtype):
+    """The batches of test_gpu_kvq.py with NaN and infinities among the new rows, in either type: what stays finite."""
+    shape, marks = SPECIAL[name]
+    c = Case(name, *shape, dtype=dtype)
+    for x, row, head, d in marks:
+        (c.k_new if x == "k" else c.v_new)[row, head, d] = 0x7E01 if dtype == "fp16" else 0x7FC1
+    print(f"[case] beside NaN {name} {dtype}", flush=True)
+    cache = c.oracle_cache()
+    dev = Device(tc, c)
+    dev.step()
+    check_cache(dev, cache, name)
+    want, bound = attention_where_finite(c, cache)
+    assert np.isfinite(bound[np.isfinite(want)]).all() and np.isnan(want).any()
+    check_attention(dev.outputs(), want, bound, name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lengths,long,waves", [("short", True, 4), ("short", False, 1), ("medium", True, 1)])
+def test_nan_among_decodes(tc, lengths, long, waves, D, dtype):
+    """NaN and infinities among new rows and older ones of decodes of one split and of several, run by workgroups and by single waves: in the rows and heads that
+    attend over them, and nowhere else."""
+    S, Hq, Hkv = 240, 32, 8
+    ctx = [(5 * i) % 50 + (i % 3 == 0) * 16 if lengths == "short" else 300 + 37 * i % 1100 for i in range(S)]
+    if long:
+        ctx[11], ctx[100], ctx[201] = 1500, 3001, 5000
+    c = Case(f"nan waves {D}", Hq, Hkv, D, [1] * S, ctx, dtype=dtype)
+    inf, nan = (0x7C00, 0x7E01) if dtype == "fp16" else (0x7F80, 0x7FC1)
+    rng = np.random.default_rng(5)
+    for i in list(range(0, S, 6)) + [11, 100, 201]:
+        x = (c.k_new, c.v_new)[i // 6 % 2]
+        x[i, rng.integers(Hkv), rng.integers(D)] = (nan, inf, inf | 0x8000)[i % 3]
+    for i in [i for i in (3, 15, 27, 100, 201) if ctx[i] > 0]:
+        for x in (c.k_hist, c.v_hist):
+            x[c.h_start[i] + rng.integers(ctx[i]), rng.integers(Hkv), rng.integers(D)] = nan
+    print(f"[case] NaN among decodes: {lengths} {long} d{D} {dtype}", flush=True)
+    cache = c.oracle_cache()
+    want, bound = attention_where_finite(c, cache)
+    bad = np.isnan(want)
+    assert bad.any((1, 2)).sum() >= 40 and not bad.all(2).all(1).any() and np.isfinite(bound[~bad]).all()
+    dev = Device(tc, c)
+    assert dev.plan.info.waves_per_item == waves and dev.plan.info.append_launch == 0 and (dev.plan.info.num_partials > 0) == long
+    dev.step()
+    check_cache(dev, cache, "step")
+    check_attention(dev.outputs(), want, bound, "step")
+    apart = Device(tc, c)
+    apart.append()
+    apart.attention()
+    assert np.array_equal(apart.outputs(), dev.outputs(), equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("S,Hq,Hkv", [(6, 8, 2), (240, 32, 8)])  # a split is run by a workgroup, by a wave
+def test_outputs_of_decodes_whose_new_values_are_large(tc, S, Hq, Hkv, dtype):
+    """New rows of V at the highest exponent of IEEE half (in bf16 at 2^100: sums of numbers of the highest are beyond 32 bits): every output, each row by a bound of its own magnitudes."""
+    c = Case(f"large {S}", Hq, Hkv, 64, [1] * S, [(5 * i) % 50 + (i % 3 == 0) * 16 for i in range(S)], dtype=dtype)
+    rng = np.random.default_rng(S)
+    for i in range(S):
+        if i % 2 == 0:
+            c.v_new[i] = bits_of((rng.standard_normal((Hkv, 64)) * (15000.0 if dtype == "fp16" else 2.0 ** 100)).astype(np.float32).clip(*(-6e4, 6e4) if dtype == "fp16" else (None, None)), dtype)
+            if dtype == "fp16":
+                c.v_new[i, 0, 5] = 0x7BFF
+    print(f"[case] large {S} {dtype}", flush=True)
+    cache = c.oracle_cache()
+    assert dtype == "bf16" or (cache.scales == 8 + 127).any()
+    dev = Device(tc, c)
+    assert (dev.plan.info.waves_per_item == 1) == (S == 240)
+    dev.step()
+    check_cache(dev, cache, "step")
+    got = dev.outputs()
+    even = np.arange(S) % 2 == 0
+    for some in (even, ~even):
+        part = copy.copy(c)
+        part.v_new = c.v_new[some]  # (the bound of IEEE half is by the largest value)
+        want, bound = part.attention(cache)
+        assert np.isfinite(want).all()
+        check_attention(got[some], want[some], bound[some], "large" if some is even else "beside")
