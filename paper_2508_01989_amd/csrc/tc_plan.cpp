@@ -5,6 +5,7 @@
 #include <chrono>
 #include <cmath>
 #include <cstring>
+#include <exception>
 #include <new>
 
 #include "tc_internal.h"
@@ -558,9 +559,8 @@ static bool append_apart_by_size(const tc_plan *p, bool chunks, int64_t pages) {
     return chunks || (p->kvq && p->waves_per_item == 1 && pages * p->Hkv * (2 * kBlock * p->D) >= (int64_t)500000000);
 }
 
-tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
-    if (!p || !pool || !b) return fail(TC_ERR_NULL, "plan, pool or batch is NULL");
-    // an error below leaves the plan describing an empty batch
+// The plan of an empty batch, but for its shape.
+static void make_empty(tc_plan *p) {
     p->S = p->T = 0;
     p->n_prefill_seqs = p->n_decode_seqs = 0;
     p->n_prefill = p->n_decode = p->n_merge = p->n_partials = p->n_piece_partials = p->n_merge_prefill = p->n_pieces = p->n_prefill_wg = p->n_counters = p->n_append = p->n_append_prefill = p->n_decode_wg = p->n_dealt = p->n_drawers = 0;
@@ -572,6 +572,9 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     p->prefill_waves = kMixedWaves;
     p->total_pages = 0;
     p->host_n = 0;
+}
+
+static tc_status build_lists(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     const int Hq = pool->num_q_heads, Hkv = pool->num_kv_heads, D = pool->head_dim;
     const bool kvq = pool->dtype >= 0 && (pool->dtype & TC_KV_E4M3);
     const int dtype = kvq ? pool->dtype & ~TC_KV_E4M3 : pool->dtype;
@@ -582,7 +585,7 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     if (Hkv > 1024) return fail(TC_ERR_SHAPE, "more than 1024 KV heads is not supported");
     const int G = Hq / Hkv;
     if (G > 16) return fail(TC_ERR_SHAPE, "more than 16 query heads per KV head is not supported");
-    if (pool->num_blocks <= 0 || pool->num_blocks * kBlock >= (int64_t)1 << 31)
+    if (pool->num_blocks <= 0 || pool->num_blocks >= ((int64_t)1 << 31) / kBlock)
         return fail(TC_ERR_SHAPE, "num_blocks must be in [1, 2^27)");
     p->Hq = Hq; p->Hkv = Hkv; p->D = D; p->G = G; p->dtype = dtype; p->kvq = kvq; p->num_blocks = pool->num_blocks;
     if (b->num_seqs < 0) return fail(TC_ERR_SPAN, "negative num_seqs");
@@ -591,9 +594,9 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     if (S > 0 && b->max_blocks <= 0) return fail(TC_ERR_BLOCK, "max_blocks must be positive");
     if (S > 0 && b->q_start[0] != 0) return fail(TC_ERR_SPAN, "q_start[0] must be 0");
 
-    p->q_start.assign(S + 1, 0);
+    p->q_start.assign((size_t)S + 1, 0);
     p->ctx_len.assign(S, 0);
-    p->page_off.assign(S + 1, 0);
+    p->page_off.assign((size_t)S + 1, 0);
     int n_prefill_seqs = 0, n_decode_seqs = 0;
     int64_t pages = 0, decode_tokens = 0;
     for (int s = 0; s < S; s++) {
@@ -1111,6 +1114,17 @@ tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
     p->off_decode = off_decode; p->off_merge = off_merge; p->off_counters = off_counters;
     p->host_n = total;
     return TC_OK;
+}
+
+tc_status build_plan(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
+    if (!p || !pool || !b) return fail(TC_ERR_NULL, "plan, pool or batch is NULL");
+    make_empty(p);  // an error leaves the plan describing an empty batch
+    try {
+        return build_lists(p, pool, b);
+    } catch (const std::exception &) {  // no memory for the lists
+        make_empty(p);
+        return fail(TC_ERR_DEVICE, "out of memory");  // (short enough to need none)
+    }
 }
 
 }  // namespace tc

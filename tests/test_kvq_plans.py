@@ -1,4 +1,8 @@
 """Plans on the CPU: what they say about batches whose tables share blocks, in 8 and in 16 bits, and the forms that chunks take in 8 bits."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 
@@ -101,3 +105,46 @@ def test_chunks_of_few_runs_a_head_are_levelled_in_8_bits(tc):
         assert (i.num_prefill_workgroups, i.block_threads) == (7 * 32, 512) and i.num_piece_partials > 0 and i.num_prefill_pieces > i.num_prefill_items
         i = chunk_form(tc, 32, 32, [chunk], decodes, bits=16)
         assert i.num_prefill_workgroups == i.num_prefill_pieces == i.num_prefill_items and i.num_piece_partials == 0
+
+
+NO_MEMORY = """
+import ctypes as C, resource, sys
+import numpy as np
+import paper_2508_01989_amd as tc
+make = getattr(tc, sys.argv[1])
+pool = make(8, 2, 128, 100)
+shape = pool.base if hasattr(pool, "base") else pool
+tc.lib()
+n = 1 << 25
+q_start, ctx, table = np.arange(n + 1, dtype=np.int32), np.zeros(n, np.int32), np.zeros((n, 1), np.int32)
+batch, keep = tc._batch(q_start, ctx, table)
+used = int(open("/proc/self/statm").read().split()[0]) * resource.getpagesize()
+p = tc.Plan(pool, [0, 1], [3], [[5]], host_only=True)
+resource.setrlimit(resource.RLIMIT_AS, (used + (64 << 20), resource.RLIM_INFINITY))
+status = tc.lib().tc_plan_update(p.handle, C.byref(shape), C.byref(batch), None)
+assert status == tc.TC_ERR_DEVICE and "memory" in tc.last_error(), (status, tc.last_error())
+other = C.c_void_p()
+assert tc.lib().tc_plan_create_host(C.byref(shape), C.byref(batch), C.byref(other)) == tc.TC_ERR_DEVICE and not other
+info = tc.tc_plan_info()
+assert tc.lib().tc_plan_get_info(p.handle, C.byref(info)) == 0 and info.num_seqs == info.total_q == info.append_launch == 0
+p.update(pool, [0, 1, 2], [3, 20], [[5, 0], [6, 7]])
+assert tc.lib().tc_plan_get_info(p.handle, C.byref(info)) == 0 and info.num_seqs == 2
+print("done")
+"""
+
+
+@pytest.mark.parametrize("make", BITS.values())
+def test_no_memory_for_a_plan_is_an_error(tc, make):
+    """Nothing throws: a batch whose lists do not fit the memory that the process may have gets a status, and the plan serves the next one."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", NO_MEMORY, make], cwd=root, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and r.stdout.strip() == "done", (r.returncode, r.stderr[-2000:])
+
+
+@pytest.mark.parametrize("bits", BITS)
+def test_pools_of_too_many_blocks_are_refused(tc, bits):
+    for nb in (1 << 27, 1 << 59, (1 << 60) + 5, (1 << 62) + 1):  # (times 16 they are 2^31, -2^63 ..)
+        with pytest.raises(tc.TcError) as e:
+            tc.Plan(getattr(tc, BITS[bits])(8, 2, 128, nb), np.zeros(1, np.int32), np.zeros(0, np.int32), np.zeros((0, 1), np.int32), host_only=True)
+        assert e.value.status == tc.TC_ERR_SHAPE
+    tc.Plan(getattr(tc, BITS[bits])(8, 2, 128, (1 << 27) - 1), np.array([0, 1]), np.array([3]), np.array([[(1 << 27) - 2]]), host_only=True)
