@@ -78,7 +78,7 @@ struct PlanScratch {
     std::vector<PlanTeam> teams;
     std::vector<int> wg_fill, open;
     std::vector<int32_t> n_teams, slot0, merge_of;
-    std::vector<uint64_t> gets_rows;  // a bit for each block of the pool, all zero between builds
+    std::vector<uint32_t> gets_rows;  // a bit for each block of the pool, all zero between builds
     std::vector<PlanUnits> units;
 };
 

@@ -978,25 +978,26 @@ static tc_status build_lists(tc_plan *p, const tc_kv_pool *pool, const tc_batch 
     // another place too, whose attention must not run beside the append.  A sum over all pages, half a nanosecond each, so only where it decides.
     p->append_apart = append_apart_by_size(p, !w.pieces.empty(), pages);
     if (kvq || !p->append_apart) {
-        if (w.gets_rows.size() * 64 < (size_t)p->num_blocks) w.gets_rows.resize(((size_t)p->num_blocks + 63) / 64, 0);
-        const auto word = [&](int32_t id) -> uint64_t & { return w.gets_rows[id >> 6]; };
+        if (w.gets_rows.size() * 32 < (size_t)p->num_blocks) w.gets_rows.resize(((size_t)p->num_blocks + 31) / 32, 0);
+        uint32_t *const bits = w.gets_rows.data();
         int64_t blocks = 0, places = 0;
         for (int64_t i = 0; i < n_append; i++) {
-            const int32_t id = H[off_append + i * kAppendInts + 3];
-            blocks += !(word(id) >> (id & 63) & 1);
-            word(id) |= (uint64_t)1 << (id & 63);
+            const uint32_t id = H[off_append + i * kAppendInts + 3];
+            blocks += !(bits[id >> 5] >> (id & 31) & 1);
+            bits[id >> 5] |= 1u << (id & 31);
         }
         p->append_shared = kvq && blocks < n_append;
         if (!p->append_apart) {
-            const uint64_t *bits = w.gets_rows.data();
             for (int s = 0; s < S; s++) {
-                const int32_t *row = b->block_table + (int64_t)s * b->max_blocks;
+                const uint32_t *row = reinterpret_cast<const uint32_t *>(b->block_table + (int64_t)s * b->max_blocks);
                 const int np = p->page_off[s + 1] - p->page_off[s];
-                for (int i = 0; i < np; i++) places += bits[row[i] >> 6] >> (row[i] & 63) & 1;
+                uint32_t found = 0;
+                for (int i = 0; i < np; i++) found += bits[row[i] >> 5] >> (row[i] & 31) & 1;
+                places += found;
             }
             p->append_apart = places > blocks;
         }
-        for (int64_t i = 0; i < n_append; i++) word(H[off_append + i * kAppendInts + 3]) = 0;
+        for (int64_t i = 0; i < n_append; i++) bits[(uint32_t)H[off_append + i * kAppendInts + 3] >> 5] = 0;
     }
 
     // ---- prefill items in `blocks` order with the KV head as the fastest index; the merge items and partial
