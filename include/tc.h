@@ -329,7 +329,7 @@ tc_status tc_probe_stream_copy(const void *src, void *dst, size_t bytes, void *s
 const char *tc_status_str(tc_status s);
 /* Text of the last error raised on the calling thread ("" if none). */
 const char *tc_last_error(void);
-int32_t tc_version(void);
+int32_t tc_version(void); /* changes with the layout of a struct */
 
 #ifdef __cplusplus
 }

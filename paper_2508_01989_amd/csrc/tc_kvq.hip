@@ -106,7 +106,8 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(uint8_t *k_pool, uint8_
         }
     }
     // ---- V.  A page that is all new goes through LDS, so that it is stored in whole pieces (a word at a time the stores of a wave touch a line four times): the eight groups
-    // of a tile lie 16 bytes further apart there, and the words that a wave stores at once are on different banks.
+    // of a tile lie 16 bytes further apart there, without which eight lanes of a store would meet on a bank.  (Two still do, 32 words apart, of the 32 lanes that it takes in at
+    // once: half of its LDS cycles are conflicts by the counter, which a kernel at the rate of a copy does not notice.)
     constexpr int kLds = CHUNK ? 8 * (2 * D + 16) : 16;  // of a wave
     const auto lds_at = [](int byte) { return byte + byte / (2 * D) * 16; };
     __shared__ __align__(16) char lds_all[4 * kLds];

@@ -180,7 +180,7 @@ static int two_split_workgroups(const tc_plan *p, int S, int split, int64_t at_o
 //   32/32 heads, one of 2157 tokens (34 pages a wave) among 29 short ones, 960 pairs 27.5 / 17.0
 static int choose_wide_split(const tc_plan *p, int S, int64_t decode_tokens) {
     const int64_t token_heads = decode_tokens * p->Hkv;
-    // (A cache in 8 bits: twice the tokens for the same bytes; us, lines at 256 / 512: 32/8 heads, 38 of 2883 43.2 / 38.3, 32/32, head_dim 64, 8 of 3571 30.0 / 27.3.)
+    // (A cache in 8 bits: twice the tokens for the same bytes; us, two batches between the lines of 256 / 512 tokens a split: 32/8 heads, 38 of 2883 43.2 / 38.3, 32/32, head_dim 64, 8 of 3571 30.0 / 27.3.)
     if (token_heads >= (int64_t)kNumCu * kDecodeWgPerCu * kDecodeWaves * (p->kvq ? 512 : 256)) return 0;
     const int split = choose_split(token_heads);  // of the single-wave form
     int64_t longest = 0, longest_pages = 0;       // the longest sequence; the pages of the longest single-wave split
@@ -975,7 +975,7 @@ static tc_status build_lists(tc_plan *p, const tc_kv_pool *pool, const tc_batch 
         }
     }
     // Blocks that get rows: from two places of the tables (in 8 bits a segment's wave rewrites the whole block, so the appends refuse that), and such that stand in
-    // another place too, whose attention must not run beside the append.  A sum over all pages, half a nanosecond each, so only where it decides.
+    // another place too, whose attention must not run beside the append.  A sum over all pages, 0.3-0.5 ns each, so only where it decides.
     p->append_apart = append_apart_by_size(p, !w.pieces.empty(), pages);
     if (kvq || !p->append_apart) {
         if (w.gets_rows.size() * 32 < (size_t)p->num_blocks) w.gets_rows.resize(((size_t)p->num_blocks + 31) / 32, 0);
@@ -1253,6 +1253,6 @@ const char *tc_status_str(tc_status s) {
 
 const char *tc_last_error(void) { return tc::g_last_error.c_str(); }
 
-int32_t tc_version(void) { return 2; }
+int32_t tc_version(void) { return 3; }
 
 }  // extern "C"

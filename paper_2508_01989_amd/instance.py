@@ -200,7 +200,8 @@ class Instance:
 
 
 class Cluster:
-    """Proxy plus instances.  kinds / chunks / blocks: one entry per instance; kvq: one too, or the same for all."""
+    """Proxy plus instances.  kinds / chunks / blocks: one entry per instance; kvq: one too, or the same for all.  cm, the cost model, is the
+    same for all instances, whichever kind of cache they have."""
 
     def __init__(self, kinds, chunks, blocks, shape, layers, cm, tpot_slo, ttft_slo, alpha=0.96, watermark_frac=0.95,
                  link_bytes_per_s=150e9, dry=False, kvq=False):
