@@ -282,6 +282,32 @@ tc_status tc_kvq_mixed_attention_append(const tc_plan *plan, const tc_kvq_pool *
                                         const void *v_new, void *out, float scale, void *workspace, size_t workspace_bytes,
                                         void *stream);
 
+/*
+ * The rows on their way into attention: the projections' q, k and v of a batch become what is attended with and cached.  Each head
+ * x of q and k is divided by its root mean square and multiplied by a weight for each element, y = x (mean(x^2) + eps)^-1/2 w, and the
+ * first rotary_dim elements of y are rotated by the row's position: pair i of them by the angle position * freq[i],
+ * (a, b) -> (a cos - b sin, b cos + a sin).  Angles are taken in 64 bits, the rest in 32, and the result is rounded once, to nearest even.  v is copied.
+ */
+typedef struct {
+    const void *q, *k, *v;                 /* DEVICE rows of the batch's tokens, a token's heads adjacent: [Hq][D], [Hkv][D], [Hkv][D] elements */
+    int64_t q_stride, k_stride, v_stride;  /* elements from a token's heads to the next token's (multiples of 8): rows may lie in one tensor  */
+    const void *q_weight, *k_weight;       /* DEVICE [D] elements, or NULL: that one is not normalised                                  */
+    float eps;                             /* positive and finite where there is a weight                                               */
+    int32_t rotary_dim;                    /* a multiple of 8 from 0 (no rotation) to D; the elements behind are not rotated            */
+    const double *freq;                    /* DEVICE [rotary_dim / 2], radians a position                                               */
+    int32_t adjacent;                      /* pair i is elements (i, i + rotary_dim / 2), or with adjacent != 0 (2 i, 2 i + 1)          */
+    const int32_t *positions;              /* DEVICE [T] positions of the rows, or NULL: those of the plan (ctx_len[s] + i)             */
+} tc_qkv_rows;
+
+/* q_out DEVICE [T][Hq][D], k_out DEVICE [T][Hkv][D]; v is not used.  Rows that are packed already may be their own output (q_out = q, k_out = k).
+ * Serves plans of either kind of cache: k_out and v are what the appends of both take.
+ * q, k, v, the weights and the outputs are 16-byte aligned (TC_ERR_ARG), and the current device is the plan's (TC_ERR_DEVICE). */
+tc_status tc_qk_norm_rotate(const tc_plan *plan, const tc_qkv_rows *rows, void *q_out, void *k_out, void *stream);
+
+/* The same, with k and v stored into the pool in the one launch: q_out and pool are bit for bit those of tc_qk_norm_rotate followed by
+ * tc_kv_append of k_out and v.  Pools 16-byte aligned.  Plans for pools in 16 bits. */
+tc_status tc_qk_norm_rotate_append(const tc_plan *plan, const tc_kv_pool *pool, const tc_qkv_rows *rows, void *q_out, void *stream);
+
 /* Test hook: un-paged copy of tokens 0..ctx+q_len-1 of sequence `seq` out of the pool,
  * k_out / v_out DEVICE [kv_len][Hkv][D] bf16. */
 tc_status tc_kv_gather(const tc_plan *plan, const tc_kv_pool *pool, int32_t seq, void *k_out, void *v_out,

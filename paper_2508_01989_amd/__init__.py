@@ -20,6 +20,7 @@ EXPORTS = ["tc_plan_create", "tc_plan_create_host", "tc_plan_update", "tc_plan_g
            "tc_plan_workspace_bytes", "tc_plan_destroy", "tc_kv_append", "tc_mixed_attention", "tc_mixed_attention_append",
            "tc_mixed_attention_static", "tc_attention_partials", "tc_split_merge",
            "tc_kv_gather", "tc_probe_mfma_loop", "tc_probe_stream_read", "tc_probe_stream_copy",
+           "tc_qk_norm_rotate", "tc_qk_norm_rotate_append",
            "tc_kvq_append", "tc_kvq_read", "tc_kvq_mixed_attention", "tc_kvq_mixed_attention_append",
            "tc_kv_transfer_bytes", "tc_kv_export", "tc_kv_import", "tc_status_str", "tc_last_error", "tc_version"]
 
@@ -32,6 +33,12 @@ class tc_kv_pool(C.Structure):
 
 class tc_kvq_pool(C.Structure):
     _fields_ = [("base", tc_kv_pool), ("scales", C.c_void_p)]
+
+
+class tc_qkv_rows(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("v_stride", C.c_int64), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float), ("rotary_dim", C.c_int32),
+                ("freq", C.c_void_p), ("adjacent", C.c_int32), ("positions", C.c_void_p)]
 
 
 class tc_batch(C.Structure):
@@ -90,6 +97,8 @@ def lib():
         L.tc_kvq_read.argtypes = [vp, C.POINTER(tc_kvq_pool), C.c_int32, vp, vp, vp]
         L.tc_kvq_mixed_attention.argtypes = [vp, C.POINTER(tc_kvq_pool), vp, vp, C.c_float, vp, C.c_size_t, vp]
         L.tc_kvq_mixed_attention_append.argtypes = [vp, C.POINTER(tc_kvq_pool), vp, vp, vp, vp, C.c_float, vp, C.c_size_t, vp]
+        L.tc_qk_norm_rotate.argtypes = [vp, C.POINTER(tc_qkv_rows), vp, vp, vp]
+        L.tc_qk_norm_rotate_append.argtypes = [vp, C.POINTER(tc_kv_pool), C.POINTER(tc_qkv_rows), vp, vp]
         L.tc_kv_transfer_bytes.argtypes = [vp, C.c_int32, C.c_int32]
         L.tc_kv_transfer_bytes.restype = C.c_size_t
         L.tc_kv_export.argtypes = [vp, C.POINTER(tc_kv_pool), C.c_int32, C.c_int32, C.POINTER(vp), C.POINTER(vp), vp, vp]
@@ -142,6 +151,23 @@ def make_kvq_pool(num_q_heads, num_kv_heads, head_dim, num_blocks, k_pool=None, 
     """A cache in 8 bits; `dtype` is the element type of q, k_new, v_new and out.  Plan takes it as it takes a tc_kv_pool."""
     return tc_kvq_pool(make_pool(num_q_heads, num_kv_heads, head_dim, num_blocks, k_pool, v_pool, block_size, dtype | TC_KV_E4M3),
                        _ptr(scales))
+
+
+def make_qkv_rows(q, k, v=None, q_weight=None, k_weight=None, eps=1e-6, freq=None, rotary_dim=None, adjacent=False, positions=None,
+                  q_stride=None, k_stride=None, v_stride=None) -> tc_qkv_rows:
+    """Rows for tc_qk_norm_rotate: tensors [T][heads][D] whose heads are adjacent; a stride that is not given is the tensor's own.  rotary_dim: twice the length of freq unless given."""
+    def stride(x, given):
+        if given is not None:
+            return int(given)
+        if x is None or isinstance(x, int):
+            return 0
+        if x.dim() == 3 and (x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2])):
+            raise ValueError("a token's heads must be adjacent")
+        return x.stride(0)
+    if rotary_dim is None:
+        rotary_dim = 0 if freq is None else 2 * freq.numel()
+    return tc_qkv_rows(_ptr(q), _ptr(k), _ptr(v), stride(q, q_stride), stride(k, k_stride), stride(v, v_stride), _ptr(q_weight), _ptr(k_weight),
+                       eps, rotary_dim, _ptr(freq), int(adjacent), _ptr(positions))
 
 
 def _shape(pool):
@@ -284,6 +310,14 @@ def tc_kvq_mixed_attention_append(plan: Plan, pool: tc_kvq_pool, q, k_new, v_new
         workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib().tc_kvq_mixed_attention_append(plan.handle, C.byref(pool), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out),
                                                C.c_float(scale), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def tc_qk_norm_rotate(plan: Plan, rows: tc_qkv_rows, q_out, k_out, stream=None):
+    _check(lib().tc_qk_norm_rotate(plan.handle, C.byref(rows), _ptr(q_out), _ptr(k_out), _stream(stream)))
+
+
+def tc_qk_norm_rotate_append(plan: Plan, pool: tc_kv_pool, rows: tc_qkv_rows, q_out, stream=None):
+    _check(lib().tc_qk_norm_rotate_append(plan.handle, C.byref(pool), C.byref(rows), _ptr(q_out), _stream(stream)))
 
 
 def _ptr_array(pools):

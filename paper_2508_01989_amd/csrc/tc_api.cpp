@@ -5,6 +5,8 @@
 
 namespace {
 
+bool misaligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
 tc_status fail(tc_status s, const std::string &msg) {
     tc::set_error(msg);
     return s;
@@ -19,6 +21,14 @@ tc_status check_runnable(const tc_plan *plan, const tc_kv_pool *pool) {
     tc_status st = tc::check_pool_matches(plan, pool, true);
     if (st != TC_OK) return st;
     if (!plan->dev) return fail(TC_ERR_ARG, "plan was built host-only (tc_plan_create_host) and cannot be launched");
+    return TC_OK;
+}
+
+tc_status check_plan_device(const tc_plan *plan) {  // last, so that a plan without a device copy shows every other mistake
+    if (!plan->dev) return fail(TC_ERR_ARG, "plan was built host-only (tc_plan_create_host) and cannot be launched");
+    int device = -1;
+    if (int err = tc::current_device(&device)) return device_result(err, "current device");
+    if (device != plan->device) return fail(TC_ERR_DEVICE, "the current device is not the one the plan was made on");
     return TC_OK;
 }
 
@@ -181,8 +191,6 @@ tc_status tc_kv_import(const tc_plan *plan, const tc_kv_pool *pool, int32_t seq,
 
 namespace {
 
-bool misaligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
-
 tc_status check_kvq(const tc_plan *plan, const tc_kvq_pool *pool) {
     if (!plan || !pool) return fail(TC_ERR_NULL, "plan or pool is NULL");
     tc_status st = tc::check_pool_matches(plan, &pool->base, true, true);
@@ -190,14 +198,6 @@ tc_status check_kvq(const tc_plan *plan, const tc_kvq_pool *pool) {
     if (!pool->scales) return fail(TC_ERR_NULL, "scales is NULL");
     if (misaligned(pool->base.k_pool, 16) || misaligned(pool->base.v_pool, 16) || misaligned(pool->scales, 2))
         return fail(TC_ERR_ARG, "k_pool and v_pool must be 16-byte aligned, scales 2-byte");
-    return TC_OK;
-}
-
-tc_status check_kvq_device(const tc_plan *plan) {  // last, so that a plan without a device copy shows every other mistake
-    if (!plan->dev) return fail(TC_ERR_ARG, "plan was built host-only (tc_plan_create_host) and cannot be launched");
-    int device = -1;
-    if (int err = tc::current_device(&device)) return device_result(err, "current device");
-    if (device != plan->device) return fail(TC_ERR_DEVICE, "the current device is not the one the plan was made on");
     return TC_OK;
 }
 
@@ -225,7 +225,7 @@ extern "C" {
 tc_status tc_kvq_append(const tc_plan *plan, const tc_kvq_pool *pool, const void *k_new, const void *v_new, void *stream) {
     tc_status st = check_kvq(plan, pool);
     if (st != TC_OK || plan->T == 0) return st;
-    if ((st = check_kvq_rows(plan, k_new, v_new)) != TC_OK || (st = check_kvq_device(plan)) != TC_OK) return st;
+    if ((st = check_kvq_rows(plan, k_new, v_new)) != TC_OK || (st = check_plan_device(plan)) != TC_OK) return st;
     return device_result(tc::launch_kvq_append(plan, pool, k_new, v_new, stream), "tc_kvq_append launch");
 }
 
@@ -242,7 +242,7 @@ tc_status tc_kvq_read(const tc_plan *plan, const tc_kvq_pool *pool, int32_t seq,
         for (int s = 0; s < plan->S; s++) tokens += plan->ctx_len[s];
         if (tokens >= (int64_t)1 << 31) return fail(TC_ERR_ARG, "2^31 tokens or more: read the sequences one by one");
     }
-    if ((st = check_kvq_device(plan)) != TC_OK) return st;
+    if ((st = check_plan_device(plan)) != TC_OK) return st;
     return device_result(tc::launch_kvq_read(plan, pool, page0, n, k_out, v_out, stream), "tc_kvq_read launch");
 }
 
@@ -250,7 +250,7 @@ tc_status tc_kvq_mixed_attention(const tc_plan *plan, const tc_kvq_pool *pool, c
                                  size_t workspace_bytes, void *stream) {
     tc_status st = check_kvq(plan, pool);
     if (st != TC_OK || plan->T == 0) return st;
-    if ((st = check_kvq_attention(plan, q, out, scale, workspace, workspace_bytes)) != TC_OK || (st = check_kvq_device(plan)) != TC_OK) return st;
+    if ((st = check_kvq_attention(plan, q, out, scale, workspace, workspace_bytes)) != TC_OK || (st = check_plan_device(plan)) != TC_OK) return st;
     return device_result(tc::launch_kvq_attention(plan, pool, q, nullptr, nullptr, out, scale, workspace, stream), "tc_kvq_mixed_attention launch");
 }
 
@@ -259,7 +259,7 @@ tc_status tc_kvq_mixed_attention_append(const tc_plan *plan, const tc_kvq_pool *
     tc_status st = check_kvq(plan, pool);
     if (st != TC_OK || plan->T == 0) return st;
     if ((st = check_kvq_rows(plan, k_new, v_new)) != TC_OK) return st;
-    if ((st = check_kvq_attention(plan, q, out, scale, workspace, workspace_bytes)) != TC_OK || (st = check_kvq_device(plan)) != TC_OK) return st;
+    if ((st = check_kvq_attention(plan, q, out, scale, workspace, workspace_bytes)) != TC_OK || (st = check_plan_device(plan)) != TC_OK) return st;
     const bool apart = plan->append_apart;
     if (apart) {
         st = device_result(tc::launch_kvq_append(plan, pool, k_new, v_new, stream), "tc_kvq_mixed_attention_append launch");
@@ -267,6 +267,56 @@ tc_status tc_kvq_mixed_attention_append(const tc_plan *plan, const tc_kvq_pool *
     }
     return device_result(tc::launch_kvq_attention(plan, pool, q, apart ? nullptr : k_new, apart ? nullptr : v_new, out, scale, workspace, stream),
                          "tc_kvq_mixed_attention_append launch");
+}
+
+}  // extern "C"
+
+// ---- norm and rotation of the rows
+
+namespace {
+
+tc_status check_rows(const tc_plan *plan, const tc_qkv_rows *rows, bool needs_v) {
+    if (rows->rotary_dim < 0 || rows->rotary_dim > plan->D || rows->rotary_dim % 8)
+        return fail(TC_ERR_SHAPE, "rotary_dim must be a multiple of 8 from 0 to head_dim");
+    if (!rows->q || !rows->k || (needs_v && !rows->v)) return fail(TC_ERR_NULL, "q, k or v is NULL");
+    if (rows->rotary_dim > 0 && !rows->freq) return fail(TC_ERR_NULL, "freq is NULL");
+    if (misaligned(rows->q, 16) || misaligned(rows->k, 16) || (needs_v && misaligned(rows->v, 16)))
+        return fail(TC_ERR_ARG, "q, k and v must be 16-byte aligned");
+    if (misaligned(rows->q_weight, 16) || misaligned(rows->k_weight, 16) || misaligned(rows->freq, 8) || misaligned(rows->positions, 4))
+        return fail(TC_ERR_ARG, "weights must be 16-byte aligned, freq 8-byte, positions 4-byte");
+    const int64_t q_row = (int64_t)plan->Hq * plan->D, kv_row = (int64_t)plan->Hkv * plan->D;
+    if (rows->q_stride < q_row || rows->k_stride < kv_row || (needs_v && rows->v_stride < kv_row))
+        return fail(TC_ERR_ARG, "a stride is smaller than a token's heads");
+    if (rows->q_stride % 8 || rows->k_stride % 8 || (needs_v && rows->v_stride % 8)) return fail(TC_ERR_ARG, "strides must be multiples of 8 elements");
+    if ((rows->q_weight || rows->k_weight) && (!(rows->eps > 0.f) || rows->eps > 3.0e38f)) return fail(TC_ERR_ARG, "eps must be positive and finite");
+    return TC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+tc_status tc_qk_norm_rotate(const tc_plan *plan, const tc_qkv_rows *rows, void *q_out, void *k_out, void *stream) {
+    if (!plan || !rows) return fail(TC_ERR_NULL, "plan or rows is NULL");
+    if (plan->T == 0) return TC_OK;
+    tc_status st = check_rows(plan, rows, false);
+    if (st != TC_OK) return st;
+    if (!q_out || !k_out) return fail(TC_ERR_NULL, "q_out or k_out is NULL");
+    if (misaligned(q_out, 16) || misaligned(k_out, 16)) return fail(TC_ERR_ARG, "q_out and k_out must be 16-byte aligned");
+    if ((st = check_plan_device(plan)) != TC_OK) return st;
+    return device_result(tc::launch_rows(plan, nullptr, rows, q_out, k_out, stream), "tc_qk_norm_rotate launch");
+}
+
+tc_status tc_qk_norm_rotate_append(const tc_plan *plan, const tc_kv_pool *pool, const tc_qkv_rows *rows, void *q_out, void *stream) {
+    if (!rows) return fail(TC_ERR_NULL, "rows is NULL");
+    tc_status st = tc::check_pool_matches(plan, pool, true);
+    if (st != TC_OK || plan->T == 0) return st;
+    if ((st = check_rows(plan, rows, true)) != TC_OK) return st;
+    if (!q_out) return fail(TC_ERR_NULL, "q_out is NULL");
+    if (misaligned(q_out, 16)) return fail(TC_ERR_ARG, "q_out must be 16-byte aligned");
+    if (misaligned(pool->k_pool, 16) || misaligned(pool->v_pool, 16)) return fail(TC_ERR_ARG, "k_pool and v_pool must be 16-byte aligned");
+    if ((st = check_plan_device(plan)) != TC_OK) return st;
+    return device_result(tc::launch_rows(plan, pool, rows, q_out, nullptr, stream), "tc_qk_norm_rotate_append launch");
 }
 
 }  // extern "C"

@@ -114,7 +114,7 @@ struct tc_plan {
     size_t host_n = 0, host_cap = 0;
     bool host_pinned = false;
     size_t off_records = 0, off_append = 0, off_pages = 0, off_valid = 0, off_rows = 0, off_prefill = 0, off_decode = 0, off_merge = 0,
-           off_counters = 0;  // off_valid: tokens (1..16) each page holds; off_rows (pools of 8 bits): tokens before it, of all sequences
+           off_counters = 0, off_seg_pos = 0;  // off_valid: tokens (1..16) each page holds; off_rows (pools of 8 bits): tokens before it, of all sequences; off_seg_pos: position of each append segment's first row
     int n_append = 0;  // (sequence, page) segments written by the append
     int n_append_prefill = 0;  // the first of them are those of the prefill chunks
     bool on_device = false;  // the plan keeps a device copy (tc_plan_create); false for tc_plan_create_host
@@ -167,6 +167,8 @@ int launch_kvq_read(const tc_plan *p, const tc_kvq_pool *pool, int page0, int n_
 // k_new / v_new non-null (not where the rows are stored apart): the kernel also stores the rows.
 int launch_kvq_attention(const tc_plan *p, const tc_kvq_pool *pool, const void *q, const void *k_new, const void *v_new, void *out, float scale, void *workspace,
                          void *stream);
+// Norm and rotation of the rows of q and k (tc_rows.hip); pool non-null: k and v are stored into it, else k goes to k_out.
+int launch_rows(const tc_plan *p, const tc_kv_pool *pool, const tc_qkv_rows *rows, void *q_out, void *k_out, void *stream);
 int current_device(int *device);
 // Host image of a plan: wait until the latest upload has read it, then make room for n int32 (pinned
 // memory when the plan has a device copy).

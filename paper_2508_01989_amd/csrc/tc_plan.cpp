@@ -932,7 +932,8 @@ static tc_status build_lists(tc_plan *p, const tc_kv_pool *pool, const tc_batch 
     while (counter_stride > 1 && n_counters * counter_stride > kCounterInts) counter_stride /= 2;
     const size_t off_queue = ((size_t)n_counters * counter_stride + kCounterLine - 1) / kCounterLine * kCounterLine;  // from off_counters
     const size_t n_counter_ints = queue || late_queue ? off_queue + kCounterLine : (size_t)n_counters * counter_stride;
-    const size_t total = std::max<size_t>(off_counters + n_counter_ints, 1);
+    const size_t off_seg_pos = off_counters + n_counter_ints;
+    const size_t total = std::max<size_t>(off_seg_pos + (size_t)n_append, 1);
     if (int err = begin_plan_host(p, total)) return fail(TC_ERR_DEVICE, std::string("host buffer of the plan: ") + hip_error_text(err));
     int32_t *H = p->host;
 
@@ -955,7 +956,7 @@ static tc_status build_lists(tc_plan *p, const tc_kv_pool *pool, const tc_batch 
     }
     {   // append segments: those of the prefill chunks first (the call that fuses the append into the attention
         // kernel still stores the chunks' rows with the append kernel, and only those)
-        int32_t *ap = H + off_append;
+        int32_t *ap = H + off_append, *seg_pos = H + off_seg_pos;
         for (int pass = 0; pass < 2; pass++) {
             for (int s = 0; s < S; s++) {
                 const int q = p->q_start[s + 1] - p->q_start[s];
@@ -968,6 +969,7 @@ static tc_status build_lists(tc_plan *p, const tc_kv_pool *pool, const tc_batch 
                     const int n_tok = std::min(kBlock - tok0, q - i);
                     ap[0] = p->q_start[s] + i; ap[1] = n_tok; ap[2] = tok0; ap[3] = ids[pos / kBlock];
                     ap += kAppendInts;
+                    *seg_pos++ = (int32_t)pos;
                     i += n_tok;
                 }
             }
@@ -1112,7 +1114,7 @@ static tc_status build_lists(tc_plan *p, const tc_kv_pool *pool, const tc_batch 
     p->n_piece_partials = (int)n_piece_partials; p->n_merge_prefill = (int)n_merge_prefill;
     p->n_decode_wg = (int)n_decode_wg; p->n_dealt = (int)n_dealt; p->n_drawers = (int)n_drawers; p->counter_stride = counter_stride; p->queue_counter = queue || late_queue ? (int)off_queue : -1;
     p->off_records = off_records; p->off_append = off_append; p->off_pages = off_pages; p->off_valid = off_valid; p->off_rows = off_rows; p->off_prefill = off_prefill;
-    p->off_decode = off_decode; p->off_merge = off_merge; p->off_counters = off_counters;
+    p->off_decode = off_decode; p->off_merge = off_merge; p->off_counters = off_counters; p->off_seg_pos = off_seg_pos;
     p->host_n = total;
     return TC_OK;
 }
