@@ -927,13 +927,13 @@ static tc_status build_lists(tc_plan *p, const tc_kv_pool *pool, const tc_batch 
     const size_t off_prefill = off_rows + (kvq ? (size_t)pages : 0);
     const size_t off_decode = off_prefill + (size_t)n_prefill * kItemInts;
     const size_t off_merge = off_decode + (size_t)n_decode * kItemInts;
-    const size_t off_counters = (off_merge + (size_t)n_merge * kItemInts + kCounterLine - 1) / kCounterLine * kCounterLine;
+    const size_t off_seg_pos = off_merge + (size_t)n_merge * kItemInts;
+    const size_t off_counters = (off_seg_pos + (size_t)n_append + kCounterLine - 1) / kCounterLine * kCounterLine;
     int counter_stride = kCounterLine;
     while (counter_stride > 1 && n_counters * counter_stride > kCounterInts) counter_stride /= 2;
     const size_t off_queue = ((size_t)n_counters * counter_stride + kCounterLine - 1) / kCounterLine * kCounterLine;  // from off_counters
     const size_t n_counter_ints = queue || late_queue ? off_queue + kCounterLine : (size_t)n_counters * counter_stride;
-    const size_t off_seg_pos = off_counters + n_counter_ints;
-    const size_t total = std::max<size_t>(off_seg_pos + (size_t)n_append, 1);
+    const size_t total = std::max<size_t>(off_counters + n_counter_ints, 1);
     if (int err = begin_plan_host(p, total)) return fail(TC_ERR_DEVICE, std::string("host buffer of the plan: ") + hip_error_text(err));
     int32_t *H = p->host;
 
