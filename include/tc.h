@@ -308,6 +308,58 @@ tc_status tc_qk_norm_rotate(const tc_plan *plan, const tc_qkv_rows *rows, void *
  * tc_kv_append of k_out and v.  Pools 16-byte aligned.  Plans for pools in 16 bits. */
 tc_status tc_qk_norm_rotate_append(const tc_plan *plan, const tc_kv_pool *pool, const tc_qkv_rows *rows, void *q_out, void *stream);
 
+/*
+ * Attention over a window: row t at position p attends over the tokens j <= p of its sequence with p - j < window or j < sinks, its newest `window` tokens (itself
+ * among them) and the first ones, as in models whose layers look back a fixed distance, and in streams that outgrow what is kept.
+ * tc_plan_set_window makes the work list for the plan's batch and uploads it on `stream`; it holds until the next tc_plan_set_window or tc_plan_update of the plan
+ * (after which it is made anew; in steady state that allocates nothing).  The rules of tc_plan_update about streams and earlier calls go for it too.  The
+ * plan serves tc_mixed_attention as before, so that layers of both kinds share it.  window >= 1, sinks >= 0 (TC_ERR_ARG); plans for pools in 16 bits (TC_ERR_SHAPE).
+ *
+ * tc_window_attention is then tc_mixed_attention with that mask: same arguments, accumulation and roundings (TC_ERR_ARG before tc_plan_set_window).  Of the cache, only blocks
+ * with a token that some row attends over are read: the table's entries for the others have to be in range, but what is there may belong to anyone.  A NaN or an
+ * infinity in a token's V reaches the rows that attend over it, and no others, and so does what is in its K.  q, out, the workspace and the pools are 16-byte aligned
+ * (TC_ERR_ARG), and the current device is the plan's (TC_ERR_DEVICE).  Results are bitwise reproducible for a fixed plan.  Two calls may overlap in
+ * time if their workspaces do not.
+ */
+tc_status tc_plan_set_window(tc_plan *plan, int32_t window, int32_t sinks, void *stream);
+size_t tc_window_workspace_bytes(const tc_plan *plan);
+tc_status tc_window_attention(const tc_plan *plan, const tc_kv_pool *pool, const void *q, void *out, float scale, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/*
+ * Attention of sequences that begin with the same cached tokens: the same result as tc_mixed_attention's, up to rounding, but the K and V of what a group of sequences shares are
+ * read once for all of its rows, as one matrix product, and not once for each.  Group g is the sequences seq_start[g] .. seq_start[g + 1] - 1 of the batch
+ * (HOST [num_groups + 1], from 0 to num_seqs, strictly increasing), which share their first prefix_len[g] tokens (HOST [num_groups], a multiple of 16, 0 for a
+ * group that shares nothing): no more than any of them has cached (TC_ERR_SPAN), in the same blocks (TC_ERR_BLOCK).  Everything else is as for the window above.
+ */
+tc_status tc_plan_set_shared(tc_plan *plan, int32_t num_groups, const int32_t *seq_start, const int32_t *prefix_len, void *stream);
+size_t tc_shared_workspace_bytes(const tc_plan *plan);
+tc_status tc_shared_attention(const tc_plan *plan, const tc_kv_pool *pool, const void *q, void *out, float scale, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* The two work lists, for inspection (shared = 0: the window's, else that of the groups). */
+typedef struct {
+    int32_t ready;            /* set for the plan's batch                                                     */
+    int32_t num_sweeps;       /* records of blocks of rows, or pieces of them: a workgroup each and KV head   */
+    int32_t num_decode_items; /* padding included (whole workgroups)                                          */
+    int32_t num_merge_items;  /* > 0: a second launch combines partial results                                */
+    int32_t waves_per_item;   /* waves that share a decode item                                               */
+    int32_t grid_blocks, block_threads; /* launch shape of the first                                          */
+    int64_t num_partial_rows; /* rows of the workspace: head_dim + 2 floats each                              */
+    int64_t build_ns, upload_ns;
+} tc_span_info;
+tc_status tc_plan_get_span_info(const tc_plan *plan, int32_t shared, tc_span_info *info);
+
+/* Copy them to HOST memory.  kind 0: sweeps, 32 int32 each; 1: decode items, 16 each; 2: merge items, 16 each.  The pages of a sweep or decode item are places in a list that
+ * is made of runs of pages of a sequence: [0, a), [b, c), then page a if h, [f, b), [c, e).
+ *   sweep  {first 64-token tile of the list, end tile, a, h, first workspace row of KV head 0 (-1 = writes out), f, rows to the next KV head, b, 0, packed rows, first packed row,
+ *           position of the first row (2^30: behind all tokens), start of the sequence's pages, c, e, 0, pool blocks of the first 16 places}
+ *   decode {position, kv_head, first place, end place (the same: padding), first packed row, first workspace row (-1 = writes out), start of the sequence's pages,
+ *           (row, head) pairs, a, h, f, b, c, e}
+ *   merge  {first packed row, packed rows, then of two lists of partial results: workspace row of the first row and KV head 0, rows to the next KV head, partial results, rows
+ *           from one to the next} */
+tc_status tc_plan_copy_span(const tc_plan *plan, int32_t shared, int32_t kind, int32_t *dst, size_t cap_items);
+
 /* Test hook: un-paged copy of tokens 0..ctx+q_len-1 of sequence `seq` out of the pool,
  * k_out / v_out DEVICE [kv_len][Hkv][D] bf16. */
 tc_status tc_kv_gather(const tc_plan *plan, const tc_kv_pool *pool, int32_t seq, void *k_out, void *v_out,

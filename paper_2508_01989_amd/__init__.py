@@ -20,7 +20,8 @@ EXPORTS = ["tc_plan_create", "tc_plan_create_host", "tc_plan_update", "tc_plan_g
            "tc_plan_workspace_bytes", "tc_plan_destroy", "tc_kv_append", "tc_mixed_attention", "tc_mixed_attention_append",
            "tc_mixed_attention_static", "tc_attention_partials", "tc_split_merge",
            "tc_kv_gather", "tc_probe_mfma_loop", "tc_probe_stream_read", "tc_probe_stream_copy",
-           "tc_qk_norm_rotate", "tc_qk_norm_rotate_append",
+           "tc_qk_norm_rotate", "tc_qk_norm_rotate_append", "tc_plan_set_window", "tc_window_workspace_bytes", "tc_window_attention",
+           "tc_plan_set_shared", "tc_shared_workspace_bytes", "tc_shared_attention", "tc_plan_get_span_info", "tc_plan_copy_span",
            "tc_kvq_append", "tc_kvq_read", "tc_kvq_mixed_attention", "tc_kvq_mixed_attention_append",
            "tc_kv_transfer_bytes", "tc_kv_export", "tc_kv_import", "tc_status_str", "tc_last_error", "tc_version"]
 
@@ -54,6 +55,11 @@ class tc_plan_info(C.Structure):
                                                       ("num_prefill_workgroups", C.c_int32), ("num_counters", C.c_int32),
                                                       ("num_piece_partials", C.c_int32), ("decode_queue", C.c_int32), ("waves_per_item", C.c_int32), ("build_ns", C.c_int64), ("upload_ns", C.c_int64),
                                                       ("append_launch", C.c_int32)]
+
+
+class tc_span_info(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("ready", "num_sweeps", "num_decode_items", "num_merge_items", "waves_per_item", "grid_blocks",
+                                         "block_threads")] + [(n, C.c_int64) for n in ("num_partial_rows", "build_ns", "upload_ns")]
 
 
 class TcError(RuntimeError):
@@ -99,6 +105,14 @@ def lib():
         L.tc_kvq_mixed_attention_append.argtypes = [vp, C.POINTER(tc_kvq_pool), vp, vp, vp, vp, C.c_float, vp, C.c_size_t, vp]
         L.tc_qk_norm_rotate.argtypes = [vp, C.POINTER(tc_qkv_rows), vp, vp, vp]
         L.tc_qk_norm_rotate_append.argtypes = [vp, C.POINTER(tc_kv_pool), C.POINTER(tc_qkv_rows), vp, vp]
+        i32p = C.POINTER(C.c_int32)
+        L.tc_plan_set_window.argtypes = [vp, C.c_int32, C.c_int32, vp]
+        L.tc_plan_set_shared.argtypes = [vp, C.c_int32, i32p, i32p, vp]
+        L.tc_window_attention.argtypes = L.tc_shared_attention.argtypes = L.tc_mixed_attention.argtypes
+        L.tc_window_workspace_bytes.argtypes = L.tc_shared_workspace_bytes.argtypes = [vp]
+        L.tc_window_workspace_bytes.restype = L.tc_shared_workspace_bytes.restype = C.c_size_t
+        L.tc_plan_get_span_info.argtypes = [vp, C.c_int32, C.POINTER(tc_span_info)]
+        L.tc_plan_copy_span.argtypes = [vp, C.c_int32, C.c_int32, i32p, C.c_size_t]
         L.tc_kv_transfer_bytes.argtypes = [vp, C.c_int32, C.c_int32]
         L.tc_kv_transfer_bytes.restype = C.c_size_t
         L.tc_kv_export.argtypes = [vp, C.POINTER(tc_kv_pool), C.c_int32, C.c_int32, C.POINTER(vp), C.POINTER(vp), vp, vp]
@@ -214,6 +228,38 @@ class Plan:
         finally:
             self._refresh()
 
+    def set_window(self, window, sinks=0, stream=None):
+        """tc_plan_set_window: this batch's work list for tc_window_attention."""
+        _check(lib().tc_plan_set_window(self.handle, int(window), int(sinks), _stream(stream)))
+
+    def set_shared(self, seq_start, prefix_len, stream=None):
+        """tc_plan_set_shared: this batch's work list for tc_shared_attention; group g is sequences seq_start[g] .. seq_start[g + 1] - 1."""
+        seq_start, prefix_len = np.ascontiguousarray(seq_start, np.int32), np.ascontiguousarray(prefix_len, np.int32)
+        if len(seq_start) != len(prefix_len) + 1:
+            raise ValueError("seq_start has one entry more than prefix_len")
+        i32p = C.POINTER(C.c_int32)
+        _check(lib().tc_plan_set_shared(self.handle, len(prefix_len), seq_start.ctypes.data_as(i32p), prefix_len.ctypes.data_as(i32p), _stream(stream)))
+
+    @property
+    def window_workspace_bytes(self) -> int:
+        return int(lib().tc_window_workspace_bytes(self.handle))
+
+    @property
+    def shared_workspace_bytes(self) -> int:
+        return int(lib().tc_shared_workspace_bytes(self.handle))
+
+    def span_info(self, shared=False) -> tc_span_info:
+        info = tc_span_info()
+        _check(lib().tc_plan_get_span_info(self.handle, int(shared), C.byref(info)))
+        return info
+
+    def span_items(self, kind: int, shared=False) -> np.ndarray:
+        info = self.span_info(shared)
+        n = (info.num_sweeps, info.num_decode_items, info.num_merge_items)[kind]
+        out = np.zeros((n, 32 if kind == 0 else 16), np.int32)
+        _check(lib().tc_plan_copy_span(self.handle, int(shared), kind, out.ctypes.data_as(C.POINTER(C.c_int32)), n))
+        return out
+
     @property
     def workspace_bytes(self) -> int:
         return int(lib().tc_plan_workspace_bytes(self.handle))
@@ -310,6 +356,18 @@ def tc_kvq_mixed_attention_append(plan: Plan, pool: tc_kvq_pool, q, k_new, v_new
         workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib().tc_kvq_mixed_attention_append(plan.handle, C.byref(pool), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out),
                                                C.c_float(scale), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def tc_window_attention(plan: Plan, pool: tc_kv_pool, q, out, scale, workspace=None, workspace_bytes=None, stream=None):
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().tc_window_attention(plan.handle, C.byref(pool), _ptr(q), _ptr(out), C.c_float(scale), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def tc_shared_attention(plan: Plan, pool: tc_kv_pool, q, out, scale, workspace=None, workspace_bytes=None, stream=None):
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().tc_shared_attention(plan.handle, C.byref(pool), _ptr(q), _ptr(out), C.c_float(scale), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def tc_qk_norm_rotate(plan: Plan, rows: tc_qkv_rows, q_out, k_out, stream=None):

@@ -12,7 +12,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtc_mi355x.so")
 SCHED_LIB = os.path.join(HERE, "libtc_sched.so")  # host-only scheduling core, built with the host compiler
-SOURCES = ["tc_plan.cpp", "tc_api.cpp", "tc_kernels.hip", "tc_kvq.hip", "tc_rows.hip", "tc_probe.hip"]
+SOURCES = ["tc_plan.cpp", "tc_api.cpp", "tc_kernels.hip", "tc_kvq.hip", "tc_rows.hip", "tc_span.hip", "tc_span_plan.cpp", "tc_probe.hip"]
 LINK_FLAGS = ["--offload-arch=gfx950", "-shared", "-fPIC", "-fno-gpu-rdc"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -320,3 +320,41 @@ tc_status tc_qk_norm_rotate_append(const tc_plan *plan, const tc_kv_pool *pool, 
 }
 
 }  // extern "C"
+
+// ---- attention over spans
+
+namespace {
+
+tc_status span_attention(const tc_plan *plan, const tc::SpanList &list, const tc_kv_pool *pool, const void *q, void *out, float scale, void *workspace, size_t workspace_bytes,
+                         void *stream, const char *no_list, const char *what) {
+    tc_status st = tc::check_pool_matches(plan, pool, true);
+    if (st != TC_OK || plan->T == 0) return st;
+    if (!list.ready) return fail(TC_ERR_ARG, no_list);
+    if (!q || !out) return fail(TC_ERR_NULL, "q or out is NULL");
+    if (misaligned(q, 16) || misaligned(out, 16)) return fail(TC_ERR_ARG, "q and out must be 16-byte aligned");
+    if (misaligned(pool->k_pool, 16) || misaligned(pool->v_pool, 16)) return fail(TC_ERR_ARG, "k_pool and v_pool must be 16-byte aligned");
+    const size_t need = plan->span_workspace_bytes(list);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return fail(TC_ERR_WORKSPACE, "workspace missing or too small");
+    if (need > 0 && misaligned(workspace, 16)) return fail(TC_ERR_ARG, "workspace must be 16-byte aligned");
+    if (!(scale > 0.f) || scale > 3.0e38f) return fail(TC_ERR_ARG, "scale must be positive and finite");
+    if ((st = check_plan_device(plan)) != TC_OK) return st;
+    return device_result(tc::launch_span(plan, list, pool, q, out, scale, workspace, stream), what);
+}
+
+}  // namespace
+
+extern "C" {
+
+tc_status tc_window_attention(const tc_plan *plan, const tc_kv_pool *pool, const void *q, void *out, float scale, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!plan) return fail(TC_ERR_NULL, "plan is NULL");
+    return span_attention(plan, plan->window, pool, q, out, scale, workspace, workspace_bytes, stream, "the plan has no window for its batch: tc_plan_set_window first",
+                          "tc_window_attention launch");
+}
+
+tc_status tc_shared_attention(const tc_plan *plan, const tc_kv_pool *pool, const void *q, void *out, float scale, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!plan) return fail(TC_ERR_NULL, "plan is NULL");
+    return span_attention(plan, plan->shared, pool, q, out, scale, workspace, workspace_bytes, stream, "the plan has no groups for its batch: tc_plan_set_shared first",
+                          "tc_shared_attention launch");
+}
+
+}  // extern "C"

@@ -42,6 +42,7 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 // round-to-nearest-even conversions of probabilities and outputs.
 struct Bf16 {
     static constexpr bool kKvq = false;
+    static constexpr uint32_t kExponentBits = 0x7F80, kExponentStep = 0x0080;
     typedef __bf16 t;
     typedef __bf16 x2 __attribute__((ext_vector_type(2)));
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
@@ -59,6 +60,7 @@ struct Bf16 {
 };
 struct Fp16 {
     static constexpr bool kKvq = false;
+    static constexpr uint32_t kExponentBits = 0x7C00, kExponentStep = 0x0400;
     typedef _Float16 t;
     typedef _Float16 x2 __attribute__((ext_vector_type(2)));
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
@@ -94,6 +96,7 @@ struct AttnArgs {
     int fused;               // 1: the last piece or team of a split pair to finish combines its partial results
     int queue;               // where the decode queue's counter (a line of its own) lies, or -1
     float scale_log2;        // softmax scale times log2(e)
+    int window, sinks;       // attention over spans: a row at position p attends over tokens j <= p with p - j < window or j < sinks
 };
 
 // Position of token `tok` (0..15) inside a 16-token row of the V pool: bits 2 and 3 exchanged, i.e.
@@ -637,6 +640,61 @@ __device__ __forceinline__ void restore_nan(const AttnArgs &A, const int32_t *__
     __syncthreads();  // the LDS is free
 }
 
+// Spans: after this thread's own direct-to-LDS loads of a page of V have landed, one that has tokens which not every row of the item attends over.  A token that
+// no row attends over becomes zero, and so does, for the rows that do not, a NaN or an infinity of any other; returns whether there was one of those: the rows
+// that do attend over it get it at the end of the sweep (span_restore).  `first`: the page's first token; the rows attend over tokens low .. last and those below `sinks`.
+template <int D, class E>
+__device__ __forceinline__ bool span_fix_v(char *lds_v, int wave, int lane, int first, int low, int last, int sinks) {
+    using C = PrefillCfg<D>;
+    constexpr uint32_t kExponent = E::kExponentBits * 0x10001u, kStep = E::kExponentStep * 0x10001u;
+    const int d = lane >> 1, half = (lane & 1) ^ ((d >> 3) & 1);
+    uint32_t seen[4];  // a mask of the two tokens in each word of the lane's eight slots
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const int a = first + v_slot(half * 8 + 2 * e), b = first + v_slot(half * 8 + 2 * e + 1);
+        seen[e] = ((a <= last && (a >= low || a < sinks)) ? 0x0000FFFFu : 0u) | ((b <= last && (b >= low || b < sinks)) ? 0xFFFF0000u : 0u);
+    }
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < C::kRuns; i++) {
+        u32x4 *piece = reinterpret_cast<u32x4 *>(lds_v + wave * C::kPageBytes + i * 1024 + lane * 16);
+        u32x4 w = *piece;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            w[e] &= seen[e];
+            const uint32_t bad = ((w[e] & kExponent) + kStep) & 0x80008000u;  // the exponent's bits all set: the sum reaches the sign's place
+            found |= bad != 0;
+            w[e] &= ~((bad >> 15) * 0xFFFFu);
+        }
+        *piece = w;
+    }
+    return found;
+}
+
+// Rare: the V of tokens that some rows of the item attend over and others do not had NaN or infinities, for which the sweep took zero.  Every lane adds those
+// that its row attends over to its accumulators (as in PiecePartial), from the pages at places [from, to) of the span.
+template <int D, class E>
+__device__ __forceinline__ void span_restore(const AttnArgs &A, const int32_t *__restrict__ pages, const SpanRuns &runs, int from, int to, int kvh, int p_abs, int low, int hh,
+                                             f32x16 (&o)[D / 32]) {
+#pragma unroll 1
+    for (int i = from; i < to; i++) {
+        const int page = runs.page(i);
+        const uint16_t *tile = A.v_pool + ((int64_t)pages[page] * A.Hkv + kvh) * (kBlock * D);
+#pragma unroll 1
+        for (int t = 0; t < kBlock; t++) {
+            const int j = page * kBlock + t;
+            const bool sees = j <= p_abs && (j >= low || j < A.sinks);
+#pragma unroll
+            for (int c = 0; c < D / 32; c++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) {
+                    const uint16_t bits = tile[(32 * c + 8 * (r >> 2) + 4 * hh + (r & 3)) * kBlock + v_slot(t)];
+                    if (sees && (bits & E::kExponentBits) == E::kExponentBits) o[c][r] += (float)__builtin_bit_cast(typename E::t, bits);
+                }
+        }
+    }
+}
+
 // max / sum across the two half-waves (lanes l and l ^ 32 hold the two halves of a row).
 __device__ __forceinline__ float half_swap_max(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -683,6 +741,14 @@ struct PrefillWave {
         for (int r = 0; r < 16; r++) {
             const int j = tok0 + 8 * (r >> 2) + 4 * hh + (r & 3);
             s[r] = (j <= p_abs) ? s[r] : -INFINITY;
+        }
+    }
+    // The same for a span: `base` are the first tokens of the half's two pages, low the first token of the row's window.
+    static __device__ __forceinline__ void span_mask(f32x16 &s, int base0, int base1, int hh, int p_abs, int low, int sinks) {
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            const int j = (r < 8 ? base0 : base1) + 8 * ((r >> 2) & 1) + 4 * hh + (r & 3);
+            s[r] = (j <= p_abs && (j >= low || j < sinks)) ? s[r] : -INFINITY;
         }
     }
     // Row maximum over the 32 tokens (both half-waves).
@@ -764,7 +830,10 @@ __device__ __forceinline__ float next_reference_max(float m_run, float row_max_l
 // a step's phases early and would wait at the barrier, so the copies cost them nothing, while waves 4-7,
 // which set the pace, are spared them (1 % on a long sweep; copies by waves 4-7 alone measured 0.2 %
 // slower than one tensor per wave group).
-template <int D, class E, int NW>
+//
+// SPAN: the same sweep over the pages of a span (SpanRuns: first the pages that all rows of the item attend over, then those that some do), for rows that
+// attend over a window of their sequence's tokens and its first ones, or over tokens that several sequences share.
+template <int D, class E, int NW, bool SPAN = false>
 __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *__restrict__ rec, int kvh, char *lds) {
     using C = PrefillCfg<D>;
     constexpr bool KVQ = E::kKvq;
@@ -784,6 +853,10 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
     const int n = lane & 31, hh = lane >> 5;
     const int pos0 = rec[RC_POS0], npos = rec[RC_NPOS], qrow0 = rec[RC_QROW0], ctx = rec[RC_CTX];
     const int n_pages = rec[RC_NPAGES];
+    static_assert(!SPAN || (!KVQ && NW == kMixedWaves));
+    SpanRuns runs = {};
+    if constexpr (SPAN) runs = {rec[SR_A], rec[SR_H], rec[SR_F], rec[SR_B], rec[SR_C], rec[SR_E]};
+    [[maybe_unused]] const int span_pages = runs.pages(), plain_tiles = runs.plain() / C::kTilePages;
     const int32_t *pages = A.pages + rec[RC_PAGEOFF];
     const int G = A.G;
     const int n_rows = npos * G;
@@ -797,7 +870,7 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
     const int wave_pmin = ctx + pos0 + min(wave * 32, n_rows - 1) / G;
     const int kv_len = ctx + pos0 + npos;  // tokens this workgroup may read (all appended already)
     // KV tiles [t_begin, t_end) of the item; region < 0: the whole range, results go to `out`
-    const int t_begin = rec[RC_T0], t_end = rec[RC_T1], region = rec[RC_REGION], p_k = rec[RC_K];
+    const int t_begin = rec[RC_T0], t_end = rec[RC_T1], region = rec[RC_REGION], p_k = SPAN ? 1 : rec[RC_K];
     const int n_sweep = t_end - t_begin;
     const float c_log2 = A.scale_log2;
     char *const lds_k = lds, *const lds_v = lds + L::kV;
@@ -839,7 +912,27 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
     int id_next[3] = {0, 0, 0};  // pages this wave copies of tiles j + 1 .. j + 3
     int window = 0;
     char *const idk_slot = lds + L::kIds + (2 * wave) * kIdSlotBytes, *const idv_slot = idk_slot + kIdSlotBytes;
-    auto page_index = [&](int tile) { return min(tile * C::kTilePages + pg, n_pages - 1); };  // past the end: the last page, whose copy is never used
+    auto page_index = [&](int tile) {  // past the end: the last page, whose copy is never used
+        if constexpr (SPAN) return runs.page(min(tile * C::kTilePages + pg, span_pages - 1));
+        else return min(tile * C::kTilePages + pg, n_pages - 1);
+    };
+    // A half-tile whose first token is `tok0` (of a span: place in its list of pages, times 16) may hold tokens that a row does not attend over.
+    [[maybe_unused]] const int low = SPAN ? p_abs - A.window + 1 : 0;
+    const auto mask = [&](f32x16 &s, int tok0) {
+        if constexpr (SPAN) W::span_mask(s, runs.first_token(tok0 / kBlock), runs.first_token(tok0 / kBlock + 1), hh, p_abs, low, A.sinks);
+        else W::causal_mask(s, tok0, hh, p_abs);
+    };
+    // The copied V of a tile with such tokens: those that no row attends over become zero (prefill_fix_tail), of a span also NaN and infinities, which are noted.
+    [[maybe_unused]] bool not_finite = false;
+    const auto fix_tail = [&](char *stage, int tile) {
+        if constexpr (SPAN) {
+            const int p_first = ctx + pos0;
+            not_finite |= span_fix_v<D, E>(stage, pg, lane, runs.first_token(tile * C::kTilePages + pg), p_first - A.window + 1, p_first + npos - 1, A.sinks);
+        } else {
+            prefill_fix_tail<D>(stage, tile, pg, lane, kv_len);
+        }
+    };
+    const auto needs_fix = [&](int tile) { return SPAN ? tile >= plain_tiles : (tile + 1) * C::kTileTokens > kv_len; };
     // The page that this wave widens in the next step, as it lies in the pool, and the exponent of its scale.
     [[maybe_unused]] uint32_t raw[KVQ ? D / 16 : 1];
     [[maybe_unused]] int raw_exponent = 0;
@@ -881,7 +974,7 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         for (int t = 0; t < NS; t++) id_next[t] = id(t + 1);
         wait_loads_but<(NS + VS - 3) * C::kRuns>();  // all but K(0) and V(0)
         if (NW == kSmallWaves) asm volatile("" : "+v"(window));  // has landed: no wait in the loop
-        if ((t_begin + 1) * C::kTileTokens > kv_len) prefill_fix_tail<D>(lds_v, t_begin, pg, lane, kv_len);
+        if (needs_fix(t_begin)) fix_tail(lds_v, t_begin);
     }
     __syncthreads();
     x8 kf[KS];     // K fragments of the half whose scores are computed next
@@ -958,14 +1051,14 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
             asm volatile("" : "+v"(pb[0]), "+v"(pb[1]), "+v"(psum));  // computed in this phase: the next one uses them
             order(std::integral_constant<int, KS>(), std::integral_constant<int, kMfma>());
             __builtin_amdgcn_sched_barrier(0);
-            if (MASK) W::causal_mask(nxt, tok_nxt, hh, p_abs);
+            if (MASK) mask(nxt, tok_nxt);
         } else {
             if (QK) W::qk(kf, qreg, nxt);
             if (KREAD) W::load_k(k_after, hk, kf);
             W::pv(vf, pb, o);
             W::load_v(v_h, hv, vf);
             W::probs(cur, c_log2, m_run, pb, psum);
-            if (MASK && QK) W::causal_mask(nxt, tok_nxt, hh, p_abs);
+            if (MASK && QK) mask(nxt, tok_nxt);
             // the probabilities are used by the next phase: have them computed in this one
             asm volatile("" : "+v"(pb[0]), "+v"(pb[1]), "+v"(psum));
         }
@@ -1016,7 +1109,7 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         pb[0] = pn[0];
         pb[1] = pn[1];
         asm volatile("" : "+v"(pb[0]), "+v"(pb[1]), "+v"(psum));  // computed in this phase: the next one uses them
-        if constexpr (decltype(mask_tag)::value) W::causal_mask(nxt, tok_nxt, hh, p_abs);
+        if constexpr (decltype(mask_tag)::value) mask(nxt, tok_nxt);
         settle(cur);
     };
     // One step for tile t_begin + j, which lives in stages s0 = j mod NS and v0 = j mod VS: `sc` holds the scores of its
@@ -1100,8 +1193,8 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         }
         if (NEXT && copier) {
             copies_landed(j);
-            if (!KVQ && decltype(mask_tag)::value && (tile + 2) * C::kTileTokens > kv_len)
-                prefill_fix_tail<D>(lds_v + v1 * C::kTileBytes, tile + 1, pg, lane, kv_len);
+            if (!KVQ && decltype(mask_tag)::value && needs_fix(tile + 1))
+                fix_tail(lds_v + v1 * C::kTileBytes, tile + 1);
         }
         s0 = s1;
         v0 = v1;
@@ -1125,8 +1218,8 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
                 copies_landed(j);
                 s0 = s0 == NS - 1 ? 0 : s0 + 1;
                 v0 = v0 == VS - 1 ? 0 : v0 + 1;
-                if (!KVQ && (t_begin + j + 2) * C::kTileTokens > kv_len)
-                    prefill_fix_tail<D>(lds_v + v0 * C::kTileBytes, t_begin + j + 1, pg, lane, kv_len);
+                if (!KVQ && needs_fix(t_begin + j + 1))
+                    fix_tail(lds_v + v0 * C::kTileBytes, t_begin + j + 1);
             }
         }
     } else {
@@ -1139,13 +1232,13 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         for (int b = 0; b < 2; b++)
 #pragma unroll
             for (int e = 0; e < 8; e++) pb[b][e] = (el)0.f;
-        if (t_begin * C::kTileTokens + 31 > wave_pmin) W::causal_mask(sc, t_begin * C::kTileTokens, hh, p_abs);
+        if (SPAN ? t_begin >= plain_tiles : t_begin * C::kTileTokens + 31 > wave_pmin) mask(sc, t_begin * C::kTileTokens);
         m_run = next_reference_max(m_run, W::row_max(sc) * c_log2);  // the first half-tile's true maxima
         const std::true_type yes;
         const std::false_type no;
         // steps 0 .. n_plain - 1 prepare tiles that lie wholly at or before every row's position
         // and before the last token: tile t needs no mask if (t + 1) * 64 - 1 <= wave_pmin
-        const int n_plain = max(0, min(n_sweep - 1, (wave_pmin + 1) / C::kTileTokens - t_begin - 1));
+        const int n_plain = max(0, min(n_sweep - 1, (SPAN ? plain_tiles : (wave_pmin + 1) / C::kTileTokens) - t_begin - 1));
         if constexpr (KVQ) {  // tile 2, for step 0, and the page id of its fetch
             wait_loads_but<TileWidener<D, E>::kLoads>();
         } else if (copier) wait_loads_but<(NS + VS - 4) * C::kRuns>();  // K(1), for step 0; the others are waited for in its end
@@ -1164,7 +1257,30 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
             restore_nan<D>(A, pages, kvh, max(t_begin * C::kTileTokens, (ctx + pos0 + 1) / C::kTileTokens * C::kTileTokens), min(t_end * C::kTileTokens, kv_len), p_abs, hh,
                            reinterpret_cast<int *>(lds), tid, NW * 64, o);
     }
-    if (NW == kMixedWaves && region >= 0) {  // (small workgroups run whole items only)
+    if constexpr (SPAN) {
+        if (t_end > plain_tiles) {  // (uniform: tiles with masked tokens were swept)
+            __syncthreads();  // every wave has left the sweep: LDS is free
+            int *const flags = reinterpret_cast<int *>(lds);
+            const bool any = __builtin_amdgcn_ballot_w64(not_finite) != 0;
+            if (lane == 0) flags[wave] = any;
+            __syncthreads();
+            if (__builtin_amdgcn_ballot_w64(flags[lane & (NW - 1)] != 0) != 0)
+                span_restore<D, E>(A, pages, runs, max(t_begin, plain_tiles) * C::kTilePages, min(t_end * C::kTilePages, span_pages), kvh, p_abs, low, hh, o);
+        }
+        if (region >= 0) {  // a partial result: rows of the workspace, as a decode unit leaves its own
+            const int64_t at = (int64_t)region + (int64_t)kvh * rec[SR_KVROWS] + R;
+            if (row_valid) {
+                float *const dst = A.ws_o + at * D + 4 * hh;
+#pragma unroll
+                for (int c = 0; c < MT; c++)
+#pragma unroll
+                    for (int q = 0; q < 4; q++)
+                        *reinterpret_cast<f32x4 *>(dst + 32 * c + 8 * q) = f32x4{o[c][4 * q], o[c][4 * q + 1], o[c][4 * q + 2], o[c][4 * q + 3]};
+                if (hh == 0) *reinterpret_cast<float2 *>(A.ws_ml + at * 2) = float2{m_run, l};
+            }
+            return;
+        }
+    } else if (NW == kMixedWaves && region >= 0) {  // (small workgroups run whole items only)
         // A piece of a cut item: every lane leaves its unnormalised accumulators, and the rows' running maximum
         // (log2 domain) and sum, in the piece's region of the workspace as they lie in registers; rows that see no
         // key of this piece carry (m, l, o) = (-1e30, 0, 0) and get weight 0 in the combination.
@@ -1406,10 +1522,11 @@ __device__ __forceinline__ void decode_fetch(const AttnArgs &A, int kvh, int id,
 
 // One page: S^T = K Q^T (16 tokens x 16 head columns, contraction over D), online softmax over the
 // 16 tokens, O^T += V^T P^T (contraction over the page's 16 tokens).
-// `exponents`: of a cache in 8 bits, those of the page's K and V scales.
-template <int D, class E>
-__device__ __forceinline__ void decode_consume(const AttnArgs &A, DecodePageOf<D, E> &st, [[maybe_unused]] int exponents, const typename E::x8 (&qreg)[D / 32],
-                                               int n_valid, int g, f32x4 (&o)[D / 16], float &m_run, float &l_run) {
+// `exponents`: of a cache in 8 bits, those of the page's K and V scales.  `mask`: puts -inf in the place of scores, and finite numbers in that of V, of
+// tokens that are not attended over.
+template <int D, class E, class Mask>
+__device__ __forceinline__ void decode_page(const AttnArgs &A, DecodePageOf<D, E> &st, [[maybe_unused]] int exponents, const typename E::x8 (&qreg)[D / 32],
+                                            f32x4 (&o)[D / 16], float &m_run, float &l_run, const Mask &mask) {
     using x8 = typename E::x8;
     using x4 = typename E::x4;
     using el = typename E::t;
@@ -1428,26 +1545,7 @@ __device__ __forceinline__ void decode_consume(const AttnArgs &A, DecodePageOf<D
         }
     }
     s += s_hi;
-    if (n_valid < kBlock) {  // the split ends inside this page: mask scores, make V finite
-#pragma unroll
-        for (int r = 0; r < 4; r++) s[r] = (4 * g + r < n_valid) ? s[r] : -INFINITY;
-        if constexpr (E::kKvq) {
-            const uint32_t real = first_bytes(n_valid - 4 * g);
-#pragma unroll
-            for (int i = 0; i < 2; i++)
-#pragma unroll
-                for (int c = 0; c < D / 32; c++) st.v[i][c] &= real;
-        } else
-#pragma unroll
-        for (int c = 0; c < MT; c++) {
-            u32x2 w = st.v[c];
-            if (4 * g + 0 >= n_valid) w[0] &= 0xFFFF0000u;
-            if (4 * g + 1 >= n_valid) w[0] &= 0x0000FFFFu;
-            if (4 * g + 2 >= n_valid) w[1] &= 0xFFFF0000u;
-            if (4 * g + 3 >= n_valid) w[1] &= 0x0000FFFFu;
-            st.v[c] = w;
-        }
-    }
+    mask(s);
     // As in the prefill branch the reference maximum of a head column (log2 domain) is kept while it serves: the page's
     // probabilities are computed against it as it is, and only when a lane's sum of its four gets out of hand (one
     // of them is above 2^11; the test also catches the first page, whose reference is -1e30, and NaN) does the wave, in
@@ -1486,6 +1584,33 @@ __device__ __forceinline__ void decode_consume(const AttnArgs &A, DecodePageOf<D
         if constexpr (E::kKvq) o[c] = E::mfma16k16(E::widen4(st.v[c & 1][c >> 1], scale_of((exponents >> 8) & 0xFF)), pb, o[c]);
         else o[c] = E::mfma16k16(__builtin_bit_cast(x4, st.v[c]), pb, o[c]);
     }
+}
+
+template <int D, class E>
+__device__ __forceinline__ void decode_consume(const AttnArgs &A, DecodePageOf<D, E> &st, int exponents, const typename E::x8 (&qreg)[D / 32], int n_valid, int g,
+                                               f32x4 (&o)[D / 16], float &m_run, float &l_run) {
+    decode_page<D, E>(A, st, exponents, qreg, o, m_run, l_run, [&](f32x4 &s) __attribute__((always_inline)) {
+        if (n_valid < kBlock) {  // the split ends inside this page: mask scores, make V finite
+#pragma unroll
+            for (int r = 0; r < 4; r++) s[r] = (4 * g + r < n_valid) ? s[r] : -INFINITY;
+            if constexpr (E::kKvq) {
+                const uint32_t real = first_bytes(n_valid - 4 * g);
+#pragma unroll
+                for (int i = 0; i < 2; i++)
+#pragma unroll
+                    for (int c = 0; c < D / 32; c++) st.v[i][c] &= real;
+            } else
+#pragma unroll
+            for (int c = 0; c < D / 16; c++) {
+                u32x2 w = st.v[c];
+                if (4 * g + 0 >= n_valid) w[0] &= 0xFFFF0000u;
+                if (4 * g + 1 >= n_valid) w[0] &= 0x0000FFFFu;
+                if (4 * g + 2 >= n_valid) w[1] &= 0xFFFF0000u;
+                if (4 * g + 3 >= n_valid) w[1] &= 0x0000FFFFu;
+                st.v[c] = w;
+            }
+        }
+    });
 }
 
 // One wave's sweep over n_pg pages (the first of them page `first_page` of the sequence) that hold n_tok tokens: the

@@ -63,6 +63,54 @@ enum { PP_ITEM, PP_T0, PP_T1, PP_SLOT, PP_K, PP_C, PP_COUNTER, PP_LAST };
 enum { RC_T0, RC_T1, RC_K, RC_C, RC_REGION, RC_COUNTER, RC_CSTRIDE, RC_NEXT, RC_POS0, RC_NPOS, RC_QROW0, RC_CTX, RC_PAGEOFF, RC_NPAGES, RC_BLOCK, RC_IDS = 16 };
 constexpr int kRecordInts = 32;
 
+// The pages of a span: what a block of rows attends over, as places in a list of pages of its sequence.  First come the pages that every row attends over
+// whole, [0, a) and [b, c), then those of which some rows do not attend over some tokens: page a if h, [f, b) and [c, e).
+#ifdef __HIPCC__
+#define TC_HOST_DEVICE __host__ __device__ inline __attribute__((always_inline))
+#else
+#define TC_HOST_DEVICE inline
+#endif
+constexpr int32_t kNoToken = 0x7FFFFFF0;  // first token of the places behind the list: past every position
+struct SpanRuns {
+    int32_t a, h, f, b, c, e;
+    TC_HOST_DEVICE int plain() const { return a + (c - b); }
+    TC_HOST_DEVICE int pages() const { return plain() + h + (b - f) + (e - c); }
+    // Page number at a place of the list, which is within it.
+    TC_HOST_DEVICE int page(int i) const {
+        if (i < a) return i;
+        i -= a;
+        if (i < c - b) return b + i;
+        i -= c - b;
+        if (i < h) return a;
+        i -= h;
+        return i < b - f ? f + i : c + i - (b - f);
+    }
+    TC_HOST_DEVICE int first_token(int i) const { return i < pages() ? page(i) * kBlock : kNoToken; }
+    // Rows at positions pos .. pos + npos - 1, each of which attends over the tokens up to its own of the newest `window` and the first `sinks`, but not of pages before `from` (at most pos / 16).
+    static TC_HOST_DEVICE SpanRuns of(int pos, int npos, int window, int sinks, int from) {
+        const int last = pos + npos - 1;
+        const int low_first = pos - window + 1 > 0 ? pos - window + 1 : 0, low_last = last - window + 1 > 0 ? last - window + 1 : 0;
+        SpanRuns r;
+        r.e = last / kBlock + 1;
+        r.c = (pos + 1) / kBlock;
+        r.f = low_first / kBlock > from ? low_first / kBlock : from;
+        r.b = (low_last + kBlock - 1) / kBlock > from ? (low_last + kBlock - 1) / kBlock : from;
+        r.a = sinks / kBlock;
+        r.h = sinks % kBlock != 0;
+        if (r.a + r.h > r.f) {  // the sinks reach into the window's first page: one run from the last whole page of sinks on
+            r.a = (sinks < pos + 1 ? sinks : pos + 1) / kBlock;
+            r.h = 0;
+            r.f = r.a;
+            if (r.b < r.a) r.b = r.a;
+        }
+        if (r.b >= r.c) r.b = r.c = r.f;  // no page that is in every row's window
+        return r;
+    }
+};
+// Pieces of the sweeps of spans are records like those of prefill pieces, with these in the fields that theirs need for other things.  REGION: row of the workspace that the
+// partial result of KV head 0 begins at, or -1; KVROWS: rows from one KV head's to the next.  POS0 is 0, CTX the position of the first row.
+enum { SR_A = RC_K, SR_H = RC_C, SR_F = RC_COUNTER, SR_KVROWS = RC_CSTRIDE, SR_B = RC_NEXT, SR_C = RC_NPAGES, SR_E = RC_BLOCK };
+
 void set_error(const std::string &msg);
 
 // Working arrays of the planner, kept in the plan so that rebuilding it for the next batch allocates nothing.
@@ -82,9 +130,61 @@ struct PlanScratch {
     std::vector<PlanUnits> units;
 };
 
+// A work list as the kernels read it: one int32 image, written on the host and uploaded as a whole.  Pinned host memory for plans with a device copy (the upload is then a
+// true asynchronous copy), plain memory otherwise.  Both buffers grow and never shrink.
+struct PlanImage {
+    int32_t *host = nullptr;
+    size_t host_n = 0, host_cap = 0;
+    bool host_pinned = false;
+    bool on_device = false;  // there is a device copy (tc_plan_create); false for tc_plan_create_host
+    int32_t *dev = nullptr;  // device copy of `host`
+    size_t dev_cap = 0;      // its capacity in int32
+    int device = -1;
+    void *upload_event = nullptr;  // hipEvent_t recorded after the latest upload: the host image may be rewritten once it has passed
+};
+
+// The work list of attention over spans of a plan's batch (tc_plan_set_window, tc_plan_set_shared).
+struct SpanBlock {  // rows that a sweep covers: npos packed rows from qrow on, the first at position pos
+    int32_t qrow, npos, pos, page_off;
+    SpanRuns runs;
+    bool partial;   // there are other partial results of these rows
+    int32_t k = 1;  // pieces
+    int64_t row0 = -1, kv_rows = 0;  // workspace row of piece 0 of KV head 0, rows from one KV head's to the next
+};
+struct SpanEntry {  // rows that decode items cover, for every KV head: `cols` (row, head) pairs
+    int32_t qrow, cols, pos, page_off;
+    SpanRuns runs;
+    bool partial;
+    int32_t units = 1;
+    int64_t row0 = -1;
+};
+struct SpanPart { int32_t qrow, n, count; int64_t row0, kv_rows, step; };  // where partial results of n packed rows lie
+constexpr int kSpanItemInts = 16;    // int32 fields of a decode item and of a merge item
+constexpr int kSpanMergeRows = 16;   // packed rows of a merge item at most
+enum { SD_POS, SD_KVH, SD_BEGIN, SD_END, SD_QROW, SD_ROW, SD_PAGEOFF, SD_COLS, SD_A, SD_H, SD_F, SD_B, SD_C, SD_E };
+enum { SM_QROW, SM_N, SM_A, SM_A_KV, SM_NA, SM_A_STEP, SM_B, SM_B_KV, SM_NB, SM_B_STEP };
+struct SpanList : PlanImage {
+    bool ready = false;  // for the plan's batch as it is
+    int window = 0, sinks = 0;
+    int n_records = 0, n_sweeps = 0, n_items = 0, n_merge = 0;  // n_sweeps: workgroups that sweep, a record for every KV head
+    int waves_log2 = 0, max_cols = 1;
+    bool wide = false;   // decodes only: fewer workgroups at a time with more pages in flight
+    int64_t n_rows = 0;  // rows of partial results in the workspace
+    size_t off_records = 0, off_items = 0, off_merge = 0;
+    int64_t build_ns = 0, upload_ns = 0;
+    int waves() const { return n_sweeps > 0 ? kMixedWaves : kDecodeWaves; }
+    int items_per_wg() const { return waves() >> waves_log2; }
+    int grid_blocks() const { return n_sweeps + n_items / items_per_wg(); }
+    // working arrays, kept so that setting the list anew allocates nothing
+    std::vector<SpanBlock> blocks;
+    std::vector<SpanEntry> entries;
+    std::vector<SpanPart> first, second;
+    std::vector<int32_t> order, records, items, merge;
+};
+
 }  // namespace tc
 
-struct tc_plan {
+struct tc_plan : tc::PlanImage {
     int Hq = 0, Hkv = 0, D = 0, G = 0;
     int dtype = TC_BF16;  // element type of q / k / v / out: selects the MFMA instantiation
     bool kvq = false;     // the pools hold 8 bits an element (TC_KV_E4M3): a plan is for one kind of pools
@@ -108,22 +208,15 @@ struct tc_plan {
     int split_tokens = 0;
     int64_t total_pages = 0;
     std::vector<int32_t> q_start, ctx_len, page_off;  // host copies
-    // One int32 image uploaded as a whole; offsets (in int32 units) of its sections.  Pinned host memory for
-    // plans with a device copy (the upload is then a true asynchronous copy), plain memory otherwise.
-    int32_t *host = nullptr;
-    size_t host_n = 0, host_cap = 0;
-    bool host_pinned = false;
+    // Offsets (in int32 units) of the sections of the image.
     size_t off_records = 0, off_append = 0, off_pages = 0, off_valid = 0, off_rows = 0, off_prefill = 0, off_decode = 0, off_merge = 0,
            off_counters = 0, off_seg_pos = 0;  // off_valid: tokens (1..16) each page holds; off_rows (pools of 8 bits): tokens before it, of all sequences; off_seg_pos: position of each append segment's first row
     int n_append = 0;  // (sequence, page) segments written by the append
     int n_append_prefill = 0;  // the first of them are those of the prefill chunks
-    bool on_device = false;  // the plan keeps a device copy (tc_plan_create); false for tc_plan_create_host
-    int32_t *dev = nullptr;  // device copy of `host`
-    size_t dev_cap = 0;      // its capacity in int32 (grows, never shrinks)
-    int device = -1;
-    void *upload_event = nullptr;  // hipEvent_t recorded after the latest upload: the host image may be rewritten once it has passed
     int64_t build_ns = 0, upload_ns = 0;  // host time of the latest work-list build and of enqueueing its upload
     tc::PlanScratch work;
+    tc::SpanList window, shared;
+    size_t span_workspace_bytes(const tc::SpanList &s) const { return s.ready ? (size_t)s.n_rows * (size_t)(D + 2) * sizeof(float) : 0; }
 
     int items_per_wg = tc::kDecodeWaves;  // decode items a workgroup runs side by side
     int prefill_waves = tc::kMixedWaves;   // waves of a workgroup beside a prefill chunk: 8, or 4 (prefill items of 128 rows)
@@ -172,9 +265,11 @@ int launch_rows(const tc_plan *p, const tc_kv_pool *pool, const tc_qkv_rows *row
 int current_device(int *device);
 // Host image of a plan: wait until the latest upload has read it, then make room for n int32 (pinned
 // memory when the plan has a device copy).
-int begin_plan_host(tc_plan *p, size_t n);
-int upload_plan(tc_plan *p, void *stream);
-void free_plan_buffers(tc_plan *p);
+int begin_plan_host(PlanImage *p, size_t n);
+int upload_plan(PlanImage *p, void *stream);
+void free_plan_buffers(PlanImage *p);
+// Attention over spans (tc_span.hip).
+int launch_span(const tc_plan *p, const SpanList &s, const tc_kv_pool *pool, const void *q, void *out, float scale, void *workspace, void *stream);
 const char *hip_error_text(int err);
 int launch_probe_mfma(int iters, void *sink, void *stream);
 int launch_probe_stream(const void *src, size_t bytes, void *sink, void *stream);

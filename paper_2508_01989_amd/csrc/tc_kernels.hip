@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(256) kv_migrate_kernel(const MigratePools pool
 int current_device(int *device) { return (int)hipGetDevice(device); }
 const char *hip_error_text(int err) { return hipGetErrorString((hipError_t)err); }
 
-int begin_plan_host(tc_plan *p, size_t n) {
+int begin_plan_host(PlanImage *p, size_t n) {
     if (p->upload_event) {
         hipError_t e = hipEventSynchronize((hipEvent_t)p->upload_event);
         if (e != hipSuccess) return (int)e;
@@ -194,7 +194,7 @@ int begin_plan_host(tc_plan *p, size_t n) {
 // Copy the host image to the device on `stream`.  The device buffer grows when a work list is larger than
 // any before it and is otherwise reused: a serving loop that keeps one plan object allocates nothing per
 // iteration.  (Growing frees the old buffer, which waits for the device to finish whatever still reads it.)
-int upload_plan(tc_plan *p, void *stream) {
+int upload_plan(PlanImage *p, void *stream) {
     int device = -1;
     hipError_t e = hipGetDevice(&device);
     if (e != hipSuccess) return (int)e;
@@ -219,7 +219,7 @@ int upload_plan(tc_plan *p, void *stream) {
     return (int)hipEventRecord((hipEvent_t)p->upload_event, (hipStream_t)stream);
 }
 
-void free_plan_buffers(tc_plan *p) {
+void free_plan_buffers(PlanImage *p) {
     if (p->upload_event) {
         (void)hipEventSynchronize((hipEvent_t)p->upload_event);
         (void)hipEventDestroy((hipEvent_t)p->upload_event);

@@ -572,6 +572,7 @@ static void make_empty(tc_plan *p) {
     p->prefill_waves = kMixedWaves;
     p->total_pages = 0;
     p->host_n = 0;
+    p->window.ready = p->shared.ready = false;
 }
 
 static tc_status build_lists(tc_plan *p, const tc_kv_pool *pool, const tc_batch *b) {
@@ -1235,6 +1236,8 @@ size_t tc_plan_workspace_bytes(const tc_plan *p) { return p ? p->workspace_bytes
 
 void tc_plan_destroy(tc_plan *p) {
     if (!p) return;
+    tc::free_plan_buffers(&p->window);
+    tc::free_plan_buffers(&p->shared);
     tc::free_plan_buffers(p);
     delete p;
 }
