@@ -140,13 +140,10 @@ def _check(status):
 
 def _ptr(x):
     """Device (or host) address of a torch tensor / numpy array / int / None."""
-    if x is None:
-        return None
-    if isinstance(x, int):
-        return x
-    if hasattr(x, "data_ptr"):
+    try:
         return x.data_ptr()
-    return x.ctypes.data
+    except AttributeError:
+        return x if x is None or isinstance(x, int) else x.ctypes.data
 
 
 def _stream(stream):
@@ -167,21 +164,23 @@ def make_kvq_pool(num_q_heads, num_kv_heads, head_dim, num_blocks, k_pool=None, 
                        _ptr(scales))
 
 
+def _row_stride(x):
+    """Elements from a token's heads to the next token's in a tensor [T][heads][D]; 0 for None or an address."""
+    if x is None or isinstance(x, int):
+        return 0
+    strides = x.stride()
+    if len(strides) == 3 and (strides[1] != x.shape[2] or strides[2] != 1) and (strides[2] != 1 or x.shape[1] > 1):
+        raise ValueError("a token's heads must be adjacent")
+    return strides[0]
+
+
 def make_qkv_rows(q, k, v=None, q_weight=None, k_weight=None, eps=1e-6, freq=None, rotary_dim=None, adjacent=False, positions=None,
                   q_stride=None, k_stride=None, v_stride=None) -> tc_qkv_rows:
     """Rows for tc_qk_norm_rotate: tensors [T][heads][D] whose heads are adjacent; a stride that is not given is the tensor's own.  rotary_dim: twice the length of freq unless given."""
-    def stride(x, given):
-        if given is not None:
-            return int(given)
-        if x is None or isinstance(x, int):
-            return 0
-        if x.dim() == 3 and (x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2])):
-            raise ValueError("a token's heads must be adjacent")
-        return x.stride(0)
     if rotary_dim is None:
         rotary_dim = 0 if freq is None else 2 * freq.numel()
-    return tc_qkv_rows(_ptr(q), _ptr(k), _ptr(v), stride(q, q_stride), stride(k, k_stride), stride(v, v_stride), _ptr(q_weight), _ptr(k_weight),
-                       eps, rotary_dim, _ptr(freq), int(adjacent), _ptr(positions))
+    return tc_qkv_rows(_ptr(q), _ptr(k), _ptr(v), _row_stride(q) if q_stride is None else q_stride, _row_stride(k) if k_stride is None else k_stride,
+                       _row_stride(v) if v_stride is None else v_stride, _ptr(q_weight), _ptr(k_weight), eps, rotary_dim, _ptr(freq), adjacent, _ptr(positions))
 
 
 def _shape(pool):
