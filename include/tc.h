@@ -318,8 +318,8 @@ tc_status tc_qk_norm_rotate_append(const tc_plan *plan, const tc_kv_pool *pool, 
  * tc_window_attention is then tc_mixed_attention with that mask: same arguments, accumulation and roundings (TC_ERR_ARG before tc_plan_set_window).  Of the cache, only blocks
  * with a token that some row attends over are read: the table's entries for the others have to be in range, but what is there may belong to anyone.  A NaN or an
  * infinity in a token's V reaches the rows that attend over it, and no others, and so does what is in its K.  q, out, the workspace and the pools are 16-byte aligned
- * (TC_ERR_ARG), and the current device is the plan's (TC_ERR_DEVICE).  Results are bitwise reproducible for a fixed plan.  Two calls may overlap in
- * time if their workspaces do not.
+ * (TC_ERR_ARG), and the current device is the plan's (TC_ERR_DEVICE).  Results are bitwise reproducible for a fixed plan.  Two calls that use the same plan's list (its arrival
+ * counters) or the same workspace must not overlap in time.
  */
 tc_status tc_plan_set_window(tc_plan *plan, int32_t window, int32_t sinks, void *stream);
 size_t tc_window_workspace_bytes(const tc_plan *plan);
@@ -340,9 +340,11 @@ tc_status tc_shared_attention(const tc_plan *plan, const tc_kv_pool *pool, const
 /* The two work lists, for inspection (shared = 0: the window's, else that of the groups). */
 typedef struct {
     int32_t ready;            /* set for the plan's batch                                                     */
-    int32_t num_sweeps;       /* records of blocks of rows, or pieces of them: a workgroup each and KV head   */
+    int32_t num_sweeps;       /* records of blocks of rows, or pieces of them                                 */
+    int32_t num_sweep_workgroups; /* each runs one record or several for one KV head: workgroup w * num_kv_heads + h record w and those chained to it */
     int32_t num_decode_items; /* padding included (whole workgroups)                                          */
-    int32_t num_merge_items;  /* > 0: a second launch combines partial results                                */
+    int32_t num_merge_items;  /* rows whose partial results are combined                                      */
+    int32_t merge_launch;     /* 1: by a second launch; 0: by the last workgroup to leave one                  */
     int32_t waves_per_item;   /* waves that share a decode item                                               */
     int32_t grid_blocks, block_threads; /* launch shape of the first                                          */
     int64_t num_partial_rows; /* rows of the workspace: head_dim + 2 floats each                              */
@@ -353,9 +355,9 @@ tc_status tc_plan_get_span_info(const tc_plan *plan, int32_t shared, tc_span_inf
 /* Copy them to HOST memory.  kind 0: sweeps, 32 int32 each; 1: decode items, 16 each; 2: merge items, 16 each.  The pages of a sweep or decode item are places in a list that
  * is made of runs of pages of a sequence: [0, a), [b, c), then page a if h, [f, b), [c, e).
  *   sweep  {first 64-token tile of the list, end tile, a, h, first workspace row of KV head 0 (-1 = writes out), f, rows to the next KV head, b, 0, packed rows, first packed row,
- *           position of the first row (2^30: behind all tokens), start of the sequence's pages, c, e, 0, pool blocks of the first 16 places}
+ *           position of the first row (2^30: behind all tokens), start of the sequence's pages, c, e, the workgroup's next record or -1, pool blocks of the first 16 places}
  *   decode {position, kv_head, first place, end place (the same: padding), first packed row, first workspace row (-1 = writes out), start of the sequence's pages,
- *           (row, head) pairs, a, h, f, b, c, e}
+ *           (row, head) pairs, a, h, f, b, c, e, then where there is no second launch the merge item and its partial results}
  *   merge  {first packed row, packed rows, then of two lists of partial results: workspace row of the first row and KV head 0, rows to the next KV head, partial results, rows
  *           from one to the next} */
 tc_status tc_plan_copy_span(const tc_plan *plan, int32_t shared, int32_t kind, int32_t *dst, size_t cap_items);

@@ -58,7 +58,7 @@ class tc_plan_info(C.Structure):
 
 
 class tc_span_info(C.Structure):
-    _fields_ = [(n, C.c_int32) for n in ("ready", "num_sweeps", "num_decode_items", "num_merge_items", "waves_per_item", "grid_blocks",
+    _fields_ = [(n, C.c_int32) for n in ("ready", "num_sweeps", "num_sweep_workgroups", "num_decode_items", "num_merge_items", "merge_launch", "waves_per_item", "grid_blocks",
                                          "block_threads")] + [(n, C.c_int64) for n in ("num_partial_rows", "build_ns", "upload_ns")]
 
 

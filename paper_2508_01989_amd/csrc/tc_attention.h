@@ -853,7 +853,7 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
     const int n = lane & 31, hh = lane >> 5;
     const int pos0 = rec[RC_POS0], npos = rec[RC_NPOS], qrow0 = rec[RC_QROW0], ctx = rec[RC_CTX];
     const int n_pages = rec[RC_NPAGES];
-    static_assert(!SPAN || (!KVQ && NW == kMixedWaves));
+    static_assert(!SPAN || !KVQ);
     SpanRuns runs = {};
     if constexpr (SPAN) runs = {rec[SR_A], rec[SR_H], rec[SR_F], rec[SR_B], rec[SR_C], rec[SR_E]};
     [[maybe_unused]] const int span_pages = runs.pages(), plain_tiles = runs.plain() / C::kTilePages;

@@ -108,8 +108,9 @@ struct SpanRuns {
     }
 };
 // Pieces of the sweeps of spans are records like those of prefill pieces, with these in the fields that theirs need for other things.  REGION: row of the workspace that the
-// partial result of KV head 0 begins at, or -1; KVROWS: rows from one KV head's to the next.  POS0 is 0, CTX the position of the first row.
-enum { SR_A = RC_K, SR_H = RC_C, SR_F = RC_COUNTER, SR_KVROWS = RC_CSTRIDE, SR_B = RC_NEXT, SR_C = RC_NPAGES, SR_E = RC_BLOCK };
+// partial result of KV head 0 begins at, or -1; KVROWS: rows from one KV head's to the next.  POS0 is 0, CTX the position of the first row,
+// SR_NEXT the record of the workgroup's next piece, or -1.
+enum { SR_A = RC_K, SR_H = RC_C, SR_F = RC_COUNTER, SR_KVROWS = RC_CSTRIDE, SR_B = RC_NEXT, SR_C = RC_NPAGES, SR_E = RC_BLOCK, SR_NEXT = RC_BLOCK + 1 };
 
 void set_error(const std::string &msg);
 
@@ -158,26 +159,36 @@ struct SpanEntry {  // rows that decode items cover, for every KV head: `cols` (
     int32_t units = 1;
     int64_t row0 = -1;
 };
+struct SpanPiece { int32_t block, t0, t1, c, run; };  // tiles [t0, t1) of a block, its piece c; the pieces of a run are one workgroup's, one after the other
 struct SpanPart { int32_t qrow, n, count; int64_t row0, kv_rows, step; };  // where partial results of n packed rows lie
 constexpr int kSpanItemInts = 16;    // int32 fields of a decode item and of a merge item
+// Of a decode item whose partial results are combined by the last workgroup to leave one: MERGE is its merge item, which its arrival counter goes by, PARTS the partial results.
 constexpr int kSpanMergeRows = 16;   // packed rows of a merge item at most
-enum { SD_POS, SD_KVH, SD_BEGIN, SD_END, SD_QROW, SD_ROW, SD_PAGEOFF, SD_COLS, SD_A, SD_H, SD_F, SD_B, SD_C, SD_E };
+enum { SD_POS, SD_KVH, SD_BEGIN, SD_END, SD_QROW, SD_ROW, SD_PAGEOFF, SD_COLS, SD_A, SD_H, SD_F, SD_B, SD_C, SD_E, SD_MERGE, SD_PARTS };
 enum { SM_QROW, SM_N, SM_A, SM_A_KV, SM_NA, SM_A_STEP, SM_B, SM_B_KV, SM_NB, SM_B_STEP };
 struct SpanList : PlanImage {
     bool ready = false;  // for the plan's batch as it is
     int window = 0, sinks = 0;
-    int n_records = 0, n_sweeps = 0, n_items = 0, n_merge = 0;  // n_sweeps: workgroups that sweep, a record for every KV head
+    int n_records = 0, n_sweeps = 0, n_items = 0, n_merge = 0;  // n_sweeps: workgroups that sweep, a run of records for every KV head
     int waves_log2 = 0, max_cols = 1;
     bool wide = false;   // decodes only: fewer workgroups at a time with more pages in flight
+    int sweep_waves = kMixedWaves;  // waves of a workgroup where there are sweeps: 8, or 4 (128 rows, several workgroups to a compute unit)
+    bool fused = false;  // the last workgroup of an item to leave its partial result combines them all: no second launch
+    int counter_stride = kCounterLine;  // int32 between arrival counters, one for each merge item and KV head
+    int merge_rows = 1;  // packed rows of the largest merge item
     int64_t n_rows = 0;  // rows of partial results in the workspace
-    size_t off_records = 0, off_items = 0, off_merge = 0;
+    size_t off_records = 0, off_items = 0, off_merge = 0, off_counters = 0;
     int64_t build_ns = 0, upload_ns = 0;
-    int waves() const { return n_sweeps > 0 ? kMixedWaves : kDecodeWaves; }
+    int waves() const { return n_sweeps > 0 ? sweep_waves : kDecodeWaves; }
     int items_per_wg() const { return waves() >> waves_log2; }
-    int grid_blocks() const { return n_sweeps + n_items / items_per_wg(); }
+    int rows_per_block() const { return 32 * sweep_waves; }
+    int n_units() const { return n_items / items_per_wg(); }  // workgroups of decode items
+    int n_first = 0, n_early = 0;  // sweeps and units that the launch begins with, dealt out evenly
+    int grid_blocks() const { return n_sweeps + n_units(); }
     // working arrays, kept so that setting the list anew allocates nothing
     std::vector<SpanBlock> blocks;
     std::vector<SpanEntry> entries;
+    std::vector<SpanPiece> pieces;
     std::vector<SpanPart> first, second;
     std::vector<int32_t> order, records, items, merge;
 };

@@ -14,12 +14,14 @@ namespace {
 
 struct SpanScalars {
     int Hq, Hkv, G;
-    int n_sweeps, n_items;
+    int n_sweeps, n_first, n_early;
     int waves_log2;   // log2 of the waves that share a decode item
     int max_cols;     // (row, head) pairs of a decode item at most
     int window, sinks;
     float scale_log2;
     int64_t n_rows;   // rows of partial results
+    int32_t *counters;  // arrival counters, or null: partial results are combined by a second launch
+    int counter_stride;
 };
 
 // Bit t: the row at position p attends over token t of page `page`.
@@ -85,9 +87,51 @@ __device__ __forceinline__ void span_decode_sweep(const AttnArgs &A, int kvh, in
     l_run = half_swap_sum(l_run);
 }
 
+// Vectors of four elements v0, v0 + step, .. of the output rows of a merge item, for KV head h: each from its row's partial results, i of them in workspace row
+// base + h * kv + i * step + r for row r of the item, for either of two lists.  PEER: other compute units have stored them while this kernel runs.
+constexpr int kSpanMergeThreads = 256, kSpanMergeBatch = 4;
+template <int D, class E, bool PEER>
+__device__ __forceinline__ void span_merge_rows(const int32_t *it, int h, const float *ws, uint16_t *out, int64_t n_rows, int Hq, int G, int v0, int v_step) {
+    constexpr int VR = D / 4;
+    const float *ws_ml = ws + n_rows * D;
+    const __amdgpu_buffer_rsrc_t win = peer_window(ws, PEER ? (uint32_t)(n_rows * D * sizeof(float)) : 0u);
+    for (int v = v0; v < it[SM_N] * G * VR; v += v_step) {
+        const int r = v / VR, d = (v % VR) * 4;
+        RowSum acc = {f32x4{0.f, 0.f, 0.f, 0.f}, -1e30f, 0.f};
+        const auto add = [&](int64_t base, int n, int64_t step) {
+            for (int i0 = 0; i0 < n; i0 += kSpanMergeBatch) {
+                f32x4 o[kSpanMergeBatch];
+                float2 ml[kSpanMergeBatch];
+#pragma unroll
+                for (int u = 0; u < kSpanMergeBatch; u++) {
+                    const int64_t at = base + min(i0 + u, n - 1) * step + r;
+                    o[u] = PEER ? load4<true>(win, ws, (uint32_t)((at * D + d) * sizeof(float))) : *reinterpret_cast<const f32x4 *>(ws + at * D + d);
+                    ml[u] = load2<PEER>(ws_ml + at * 2);
+                }
+#pragma unroll
+                for (int u = 0; u < kSpanMergeBatch; u++)
+                    if (i0 + u < n) acc.add(o[u], ml[u].x, ml[u].y);
+            }
+        };
+        add((int64_t)it[SM_A] + (int64_t)h * it[SM_A_KV], it[SM_NA], it[SM_A_STEP]);
+        add((int64_t)it[SM_B] + (int64_t)h * it[SM_B_KV], it[SM_NB], it[SM_B_STEP]);
+        const float inv = 1.f / acc.l;
+        typename E::x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; e++) w[e] = (typename E::t)(acc.o[e] * inv);
+        *reinterpret_cast<typename E::x4 *>(out + ((int64_t)(it[SM_QROW] + r / G) * Hq + h * G + r % G) * D + d) = w;
+    }
+}
+
+// Workgroup (x, h, z): share z of merge item x of KV head h.
+template <int D, class E>
+__global__ void __launch_bounds__(kSpanMergeThreads) span_merge_kernel(const int32_t *__restrict__ merge, const float *__restrict__ ws, uint16_t *__restrict__ out, int64_t n_rows, int Hq, int G) {
+    span_merge_rows<D, E, false>(merge + (int64_t)blockIdx.x * kSpanItemInts, blockIdx.y, ws, out, n_rows, Hq, G, blockIdx.z * kSpanMergeThreads + threadIdx.x, gridDim.z * kSpanMergeThreads);
+}
+
 // One workgroup's decode items: WAVES >> waves_log2 of them, each run by 1 << waves_log2 waves that share its pages out in contiguous runs and meet in LDS.
 template <int D, class E, int NS, int WAVES>
-__device__ __forceinline__ void span_decode(const AttnArgs &A, const SpanScalars &sc, const int32_t *__restrict__ items, int unit, float *lds) {
+__device__ __forceinline__ void span_decode(const AttnArgs &A, const SpanScalars &sc, const int32_t *__restrict__ items, const int32_t *__restrict__ merge, int unit, float *lds) {
     using x4 = typename E::x4;
     using el = typename E::t;
     constexpr int MT = D / 16, VR = D / 4;
@@ -147,96 +191,92 @@ __device__ __forceinline__ void span_decode(const AttnArgs &A, const SpanScalars
 #pragma unroll
             for (int e = 0; e < 4; e++) w4[e] = (el)(acc[e] * inv);
             *reinterpret_cast<x4 *>(out_row(jj) + d) = w4;
+        } else if (sc.counters) {
+            peer_store4(peer_window(A.ws_o + (int64_t)row * D, (uint32_t)(cols * D * sizeof(float))), (uint32_t)v * 16, acc);
+            if (d == 0) peer_store2(A.ws_ml + ((int64_t)row + jj) * 2, m, l);
         } else {
             *reinterpret_cast<f32x4 *>(A.ws_o + ((int64_t)row + jj) * D + d) = acc;
             if (d == 0) *reinterpret_cast<float2 *>(A.ws_ml + ((int64_t)row + jj) * 2) = float2{m, l};
         }
     }
+    if (row < 0 || !sc.counters) return;
+    // (The whole workgroup runs one item.)  The last workgroup of the sequence and KV head to get here combines all partial results; nobody waits.
+    stores_done();
+    int32_t *const counter = sc.counters + (it[SD_MERGE] * A.Hkv + kvh) * sc.counter_stride;
+    if (!workgroup_arrives_last(counter, it[SD_PARTS], reinterpret_cast<int *>(lds), tid)) return;
+    span_merge_rows<D, E, true>(merge + (int64_t)it[SD_MERGE] * kSpanItemInts, kvh, A.ws_o, A.out, sc.n_rows, A.Hq, G, tid, WAVES * 64);
 }
 
-template <int D, class E, int WAVES, int PER_CU, int NS>
+template <int D, class E, int WAVES, int PER_CU, int NS, bool SWEEPS>
 __global__ void __launch_bounds__(WAVES * 64, PER_CU)
     span_attention_kernel(const uint16_t *__restrict__ k_pool, const uint16_t *__restrict__ v_pool, const uint16_t *__restrict__ q, uint16_t *__restrict__ out,
-                          const int32_t *__restrict__ pages, const int32_t *__restrict__ records, const int32_t *__restrict__ items, float *ws, const SpanScalars sc) {
+                          const int32_t *__restrict__ pages, const int32_t *__restrict__ records, const int32_t *__restrict__ items, const int32_t *__restrict__ merge, float *ws, const SpanScalars sc) {
     extern __shared__ __align__(16) char lds[];
     AttnArgs A = {};
     A.k_pool = const_cast<uint16_t *>(k_pool); A.v_pool = const_cast<uint16_t *>(v_pool); A.q = q; A.out = out; A.pages = pages;
     A.ws_o = ws; A.ws_ml = ws + sc.n_rows * D;
     A.Hq = sc.Hq; A.Hkv = sc.Hkv; A.G = sc.G; A.scale_log2 = sc.scale_log2; A.window = sc.window; A.sinks = sc.sinks;
     const int wg = (int)blockIdx.x;
-    if constexpr (WAVES == kMixedWaves) {
-        if (wg < sc.n_sweeps) {
-            prefill_item<D, E, WAVES, true>(A, records + (int64_t)(wg / A.Hkv) * kRecordInts, wg % A.Hkv, lds);
-            return;
+    int unit = wg;
+    if constexpr (SWEEPS) {
+        // The order of the launch: n_first sweeps and n_early decode units, dealt out evenly in rows of Hkv workgroups, then the other sweeps, then the other units.
+        int sweep = -1;
+        const int mixed = sc.n_first + sc.n_early;
+        if (wg < mixed) {
+            const int Hkv = A.Hkv, row = wg / Hkv, rows = mixed / Hkv, sweep_rows = sc.n_first / Hkv;
+            const int before = (int)((int64_t)row * sweep_rows / rows);  // rows of sweeps before this one
+            if ((int)((int64_t)(row + 1) * sweep_rows / rows) > before) sweep = before * Hkv + wg % Hkv;
+            else unit = (row - before) * Hkv + wg % Hkv;
+        } else if (wg < sc.n_sweeps + sc.n_early) {
+            sweep = wg - sc.n_early;
+        } else {
+            unit = wg - sc.n_sweeps;
+        }
+        if (sweep >= 0) {
+            for (int r = sweep / A.Hkv;;) {
+                const int32_t *rec = records + (int64_t)r * kRecordInts;
+                prefill_item<D, E, WAVES, true>(A, rec, sweep % A.Hkv, lds);
+                r = rec[SR_NEXT];
+                if (r < 0) return;
+                __syncthreads();  // the next piece's tile copies reuse the LDS
+            }
         }
     }
-    span_decode<D, E, NS, WAVES>(A, sc, items, wg - sc.n_sweeps, reinterpret_cast<float *>(lds));
-}
-
-// Workgroup (x, h): merge item x, up to kSpanMergeRows packed rows of one KV head h.  Partial result i of row r of the item lies in workspace row base + h * kv + i * step + r, for
-// either of two lists of them.
-constexpr int kSpanMergeThreads = 256, kSpanMergeBatch = 4;
-template <int D, class E>
-__global__ void __launch_bounds__(kSpanMergeThreads) span_merge_kernel(const int32_t *__restrict__ merge, const float *__restrict__ ws, uint16_t *__restrict__ out, int64_t n_rows, int Hq, int G) {
-    constexpr int VR = D / 4;
-    const int32_t *it = merge + (int64_t)blockIdx.x * kSpanItemInts;
-    const int h = blockIdx.y;
-    const float *ws_ml = ws + n_rows * D;
-    for (int v = threadIdx.x; v < it[SM_N] * G * VR; v += kSpanMergeThreads) {
-        const int r = v / VR, d = (v % VR) * 4;
-        RowSum acc = {f32x4{0.f, 0.f, 0.f, 0.f}, -1e30f, 0.f};
-        const auto add = [&](int64_t base, int n, int64_t step) {
-            for (int i0 = 0; i0 < n; i0 += kSpanMergeBatch) {
-                f32x4 o[kSpanMergeBatch];
-                float2 ml[kSpanMergeBatch];
-#pragma unroll
-                for (int u = 0; u < kSpanMergeBatch; u++) {
-                    const int64_t at = base + min(i0 + u, n - 1) * step + r;
-                    o[u] = *reinterpret_cast<const f32x4 *>(ws + at * D + d);
-                    ml[u] = *reinterpret_cast<const float2 *>(ws_ml + at * 2);
-                }
-#pragma unroll
-                for (int u = 0; u < kSpanMergeBatch; u++)
-                    if (i0 + u < n) acc.add(o[u], ml[u].x, ml[u].y);
-            }
-        };
-        add((int64_t)it[SM_A] + (int64_t)h * it[SM_A_KV], it[SM_NA], it[SM_A_STEP]);
-        add((int64_t)it[SM_B] + (int64_t)h * it[SM_B_KV], it[SM_NB], it[SM_B_STEP]);
-        const float inv = 1.f / acc.l;
-        typename E::x4 w;
-#pragma unroll
-        for (int e = 0; e < 4; e++) w[e] = (typename E::t)(acc.o[e] * inv);
-        *reinterpret_cast<typename E::x4 *>(out + ((int64_t)(it[SM_QROW] + r / G) * Hq + h * G + r % G) * D + d) = w;
-    }
+    span_decode<D, E, NS, WAVES>(A, sc, items, merge, unit, reinterpret_cast<float *>(lds));
 }
 
 template <int D, class E>
 int launch_span_d(const tc_plan *p, const SpanList &s, const tc_kv_pool *pool, const void *q, void *out, float scale, void *workspace, hipStream_t st) {
     const int32_t *pages = p->dev + p->off_pages, *records = s.dev + s.off_records, *items = s.dev + s.off_items, *merge = s.dev + s.off_merge;
-    const SpanScalars sc = {p->Hq, p->Hkv, p->G, s.n_sweeps, s.n_items, s.waves_log2, s.max_cols, s.window, s.sinks, scale * 1.4426950408889634f, s.n_rows};
+    const SpanScalars sc = {p->Hq, p->Hkv, p->G, s.n_sweeps, s.n_first, s.n_early, s.waves_log2, s.max_cols, s.window, s.sinks, scale * 1.4426950408889634f, s.n_rows,
+                            s.fused ? s.dev + s.off_counters : nullptr, s.counter_stride};
     const int grid = s.grid_blocks();
-    const auto launch = [&](auto waves, auto per_cu, auto stages, size_t lds) {
-        span_attention_kernel<D, E, decltype(waves)::value, decltype(per_cu)::value, decltype(stages)::value><<<grid, decltype(waves)::value * 64, lds, st>>>(
-            (const uint16_t *)pool->k_pool, (const uint16_t *)pool->v_pool, (const uint16_t *)q, (uint16_t *)out, pages, records, items, (float *)workspace, sc);
-    };
-    if (s.n_sweeps > 0) {
-        static std::atomic<bool> done[kMaxDevices];  // more than 64 KiB of LDS needs an opt-in for each device
-        const bool known = p->device >= 0 && p->device < kMaxDevices;
-        if (!known || !done[p->device].load(std::memory_order_acquire)) {
-            const hipError_t e = hipFuncSetAttribute((const void *)span_attention_kernel<D, E, kMixedWaves, 1, kDecodeStages>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                     PrefillLds<D, kMixedWaves>::kBytes);
-            if (e != hipSuccess) return (int)e;
-            if (known) done[p->device].store(true, std::memory_order_release);
+    const auto launch = [&](auto waves, auto per_cu, auto stages, auto sweeps, size_t lds) {
+        constexpr int W = decltype(waves)::value, PER_CU = decltype(per_cu)::value, NS = decltype(stages)::value;
+        constexpr bool SWEEPS = decltype(sweeps)::value;
+        if (SWEEPS) {  // more than 64 KiB of LDS needs an opt-in for each device
+            static std::atomic<bool> done[kMaxDevices];
+            const bool known = p->device >= 0 && p->device < kMaxDevices;
+            if (!known || !done[p->device].load(std::memory_order_acquire)) {
+                const hipError_t e = hipFuncSetAttribute((const void *)span_attention_kernel<D, E, W, PER_CU, NS, SWEEPS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+                if (e != hipSuccess) return (int)e;
+                if (known) done[p->device].store(true, std::memory_order_release);
+            }
         }
-        launch(Int<kMixedWaves>(), Int<1>(), Int<kDecodeStages>(), PrefillLds<D, kMixedWaves>::kBytes);
-    } else if (s.wide) {
-        launch(Int<kDecodeWaves>(), Int<2>(), Int<kWideStages>(), decode_lds_bytes(kDecodeWaves, s.max_cols, D));
-    } else {
-        launch(Int<kDecodeWaves>(), Int<kDecodeWgPerCu>(), Int<kDecodeStages>(), decode_lds_bytes(kDecodeWaves, s.max_cols, D));
-    }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || s.n_merge == 0) return (int)e;
-    span_merge_kernel<D, E><<<dim3((unsigned)s.n_merge, (unsigned)p->Hkv), kSpanMergeThreads, 0, st>>>(merge, (const float *)workspace, (uint16_t *)out, s.n_rows, p->Hq, p->G);
+        span_attention_kernel<D, E, W, PER_CU, NS, SWEEPS><<<grid, W * 64, lds, st>>>(
+            (const uint16_t *)pool->k_pool, (const uint16_t *)pool->v_pool, (const uint16_t *)q, (uint16_t *)out, pages, records, items, merge, (float *)workspace, sc);
+        return (int)hipGetLastError();
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    int err;
+    if (s.n_sweeps > 0 && s.sweep_waves == kMixedWaves) err = launch(Int<kMixedWaves>(), Int<1>(), Int<kDecodeStages>(), yes, PrefillLds<D, kMixedWaves>::kBytes);
+    else if (s.n_sweeps > 0) err = launch(Int<kSmallWaves>(), Int<small_wg_per_cu(D)>(), Int<kDecodeStages>(), yes, PrefillLds<D, kSmallWaves>::kBytes);
+    else if (s.wide) err = launch(Int<kDecodeWaves>(), Int<2>(), Int<kWideStages>(), no, decode_lds_bytes(kDecodeWaves, s.max_cols, D));
+    else err = launch(Int<kDecodeWaves>(), Int<kDecodeWgPerCu>(), Int<kDecodeStages>(), no, decode_lds_bytes(kDecodeWaves, s.max_cols, D));
+    if (err || s.n_merge == 0 || s.fused) return err;
+    const unsigned shares = (unsigned)std::max(1, s.merge_rows * p->G * (D / 4) / kSpanMergeThreads);
+    span_merge_kernel<D, E><<<dim3((unsigned)s.n_merge, (unsigned)p->Hkv, shares), kSpanMergeThreads, 0, st>>>(merge, (const float *)workspace, (uint16_t *)out, s.n_rows, p->Hq, p->G);
     return (int)hipGetLastError();
 }
 

@@ -18,16 +18,19 @@ tc_status fail(tc_status s, const char *msg) {
 
 constexpr int kTilePages = kPrefillTileTokens / kBlock;
 constexpr int kMinSweepTiles = 4;   // a piece of a cut sweep is not shorter than this
-constexpr int kMinWavePages = 4;    // nor does a wave get fewer pages of a decode item that is shared out
+constexpr double kPieceUs = 6, kMergeUs = 8;  // what a piece costs on top of its tiles: its start and end; and the launch that combines pieces
+constexpr int kUncutPages = 28, kFewUncutPages = 10;   // a wave gets up to that many before an item is cut: where uncut items fill the chip, where they do not
+constexpr int kShortSweepTiles = 32;
+constexpr int kMinWavePages = 6;    // nor does a wave get fewer pages of a decode item that is shared out
 constexpr int64_t kDecodeWaveSlots = (int64_t)kNumCu * kDecodeWgPerCu * kDecodeWaves;  // waves of decode-only workgroups that the chip holds
 // Rates that the two branches are balanced with where a batch has both (one MI355X): what a sweep of 256 rows takes for a tile, and what a compute unit streams.
-constexpr double kSweepTileUs = 1.8, kStreamCuBytesPerUs = 25e3;
+constexpr double kSweepTileUs = 1.8, kStreamCuBytesPerUs = 40e3, kStreamBytesPerUs = 6e6;
 
 int tiles_of(const SpanRuns &r) { return (r.pages() + kTilePages - 1) / kTilePages; }
 
 // Rows of one sequence (or, with `from` >= 0 and runs given by the caller, of several) in blocks that a workgroup sweeps.
 void add_blocks(const tc_plan *p, SpanList &s, int seq, int from) {
-    const int per = kPrefillRows / p->G, q = p->q_start[seq + 1] - p->q_start[seq];
+    const int per = s.rows_per_block() / p->G, q = p->q_start[seq + 1] - p->q_start[seq];
     for (int i = 0; i < q; i += per) {
         SpanBlock b;
         b.npos = std::min(per, q - i);
@@ -54,44 +57,109 @@ void add_sequence(const tc_plan *p, SpanList &s, int seq, int from) {
     else add_blocks(p, s, seq, from);
 }
 
+// The sweeps in runs of equal cost, `bins` for each KV head: the blocks laid end to end, the longest first, and cut where a run is full.
+void level(SpanList &s, int bins, double piece_tiles) {
+    s.order.resize(s.blocks.size());
+    std::iota(s.order.begin(), s.order.end(), 0);
+    std::stable_sort(s.order.begin(), s.order.end(), [&](int x, int y) { return tiles_of(s.blocks[x].runs) > tiles_of(s.blocks[y].runs); });
+    double left = (bins - 1) * piece_tiles;  // a cut makes one piece more
+    for (const SpanBlock &b : s.blocks) left += tiles_of(b.runs) + piece_tiles;
+    int run = 0;
+    double room = left / bins;
+    for (const int i : s.order) {
+        SpanBlock &b = s.blocks[i];
+        const int n = tiles_of(b.runs);
+        b.k = 0;
+        for (int at = 0; at < n;) {
+            int take = n - at;
+            const int fits = (int)(room - piece_tiles + 0.5);
+            if (run + 1 < bins && fits < take) {
+                if (fits < kMinSweepTiles && room < left / (bins - run) - 0.5) {  // too little for a piece: what is left is shared out over the other runs
+                    run++;
+                    room = left / (bins - run);
+                    continue;
+                }
+                const int cut = std::max(fits, kMinSweepTiles);
+                if (take - cut >= kMinSweepTiles) take = cut;
+            }
+            s.pieces.push_back({i, at, at + take, b.k++, run});
+            at += take;
+            room -= take + piece_tiles;
+            left -= take + piece_tiles;
+            if (run + 1 < bins && room < kMinSweepTiles) {
+                run++;
+                room = left / (bins - run);
+            }
+        }
+    }
+}
+
 // The pieces of the sweeps and the waves of the decode items.
 void share_out(const tc_plan *p, SpanList &s) {
     const int64_t Hkv = p->Hkv;
-    int64_t tiles = 0, longest = 1, pages = 0;
+    int64_t tiles = 0, longest = 0, pages = 0;
     for (const SpanBlock &b : s.blocks) {
         tiles += tiles_of(b.runs);
         longest = std::max<int64_t>(longest, tiles_of(b.runs));
     }
     for (const SpanEntry &e : s.entries) pages += e.runs.pages();
-    if (!s.blocks.empty() && (int64_t)s.blocks.size() * Hkv < kNumCu) {
-        // Few sweeps: cut, so that they take the compute units that decodes beside them leave, all of them where there are none.
-        int64_t target = kNumCu;
-        if (pages > 0) {
-            const double sweep_us = (double)tiles * Hkv * kSweepTileUs * p->D / 128, stream_us = (double)pages * Hkv * kBlock * p->token_bytes() / kStreamCuBytesPerUs;
-            target = std::max<int64_t>((int64_t)s.blocks.size() * Hkv, (int64_t)(kNumCu * sweep_us / (sweep_us + stream_us)));
-        }
-        int64_t length = std::max<int64_t>(kMinSweepTiles, tiles * Hkv / std::max<int64_t>(target, 1));
-        for (; length < longest; length++) {
-            int64_t n = 0;
-            for (const SpanBlock &b : s.blocks) n += (tiles_of(b.runs) + length - 1) / length;
-            if (n * Hkv <= target) break;
-        }
-        for (SpanBlock &b : s.blocks) b.k = (int32_t)std::max<int64_t>(1, (tiles_of(b.runs) + length - 1) / length);
-    }
     const bool sweeps = !s.blocks.empty();
-    const int waves = sweeps ? kMixedWaves : kDecodeWaves;
-    const int64_t slots = sweeps ? (int64_t)kNumCu * kMixedWaves : kDecodeWaveSlots;
-    const int64_t per_wave = std::min<int64_t>(kMaxSplitPages, std::max<int64_t>(kMinWavePages, (pages * Hkv + slots - 1) / slots));
+    const int waves = s.blocks.empty() ? kDecodeWaves : s.sweep_waves;
+    const int64_t wg_slots = sweeps ? (int64_t)kNumCu * (s.sweep_waves == kMixedWaves ? 1 : small_wg_per_cu(p->D)) : kNumCu * kDecodeWgPerCu;
+    const double tile_us = kSweepTileUs * p->D / 128 * s.sweep_waves / kMixedWaves;  // of a workgroup, per compute unit
+    const double sweep_us = ((double)tiles * tile_us + (double)s.blocks.size() * kPieceUs) * Hkv;
+    const double bytes = (double)pages * Hkv * kBlock * p->token_bytes(), stream_us = bytes / kStreamCuBytesPerUs;
+    const double share = sweep_us / std::max(1e-9, sweep_us + stream_us);  // of the compute units that sweep
+    if (sweeps) {
+        const int64_t whole = (int64_t)s.blocks.size() * Hkv;
+        const int64_t target = std::max<int64_t>(Hkv, (int64_t)((double)wg_slots * (pages > 0 ? share : 1.0)));  // workgroups that sweep at a time
+        const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(target / Hkv, tiles / kMinSweepTiles));
+        // Few blocks: whole, or in level runs, which pay a start and an end for each piece and a launch that combines them.  Not beside a stream that takes longer than the longest sweep.
+        const double per_tile = tile_us * (double)wg_slots / kNumCu, piece = kPieceUs;
+        const double t_whole = std::max((double)longest * per_tile + piece, bytes / kStreamBytesPerUs);
+        const double t_level = ((double)tiles * per_tile + (double)(s.blocks.size() + bins - 1) * piece) / (double)bins + kMergeUs;
+        if (whole < target && std::max(t_level, bytes / kStreamBytesPerUs) < 0.95 * t_whole) level(s, (int)bins, piece / per_tile);
+    }
+    if (s.pieces.empty())
+        for (size_t i = 0; i < s.blocks.size(); i++) s.pieces.push_back({(int32_t)i, 0, tiles_of(s.blocks[i].runs), 0, (int32_t)i});
+
+    // Pages of a wave: as many as keep all waves that the chip holds busy, but no fewer than are worth a wave.
+    const int64_t slots = wg_slots * waves, least = kMinWavePages;
+    const int64_t per_wave = std::min<int64_t>(kMaxSplitPages, std::max<int64_t>(least, (pages * Hkv + slots - 1) / slots));
     s.waves_log2 = 0;
     if (!s.entries.empty()) {
         const int64_t mean = (pages + (int64_t)s.entries.size() - 1) / (int64_t)s.entries.size();
         while ((1 << s.waves_log2) < waves && ((int64_t)per_wave << s.waves_log2) < mean) s.waves_log2++;
     }
     s.wide = !sweeps && (pages * Hkv + per_wave - 1) / per_wave <= (int64_t)kNumCu * 2 * kDecodeWaves;
-    // An item that is a little longer than the mean is not cut for it.
-    const int64_t most = std::min<int64_t>((int64_t)kMaxSplitPages << s.waves_log2, (int64_t)(per_wave + per_wave / 2) << s.waves_log2);
-    for (SpanEntry &e : s.entries) e.units = (int32_t)((e.runs.pages() + most - 1) / most);
+    // A sequence is cut into several items only where that saves more pages a wave than the launch that combines them costs.
+    const int64_t most = std::min<int64_t>((int64_t)kMaxSplitPages << s.waves_log2, std::max<int64_t>(per_wave + per_wave / 2, (int64_t)s.entries.size() * Hkv >= kNumCu ? kUncutPages : kFewUncutPages) << s.waves_log2);
+    int64_t n_items = 0;
+    for (SpanEntry &e : s.entries) {
+        const int64_t n = e.runs.pages(), each = e.partial ? std::min<int64_t>(per_wave + per_wave / 2, kMaxSplitPages) << s.waves_log2 : n <= most ? most : per_wave << s.waves_log2;
+        e.units = (int32_t)((n + each - 1) / each);
+        n_items += e.units * Hkv;
+    }
+    // More workgroups than the chip holds: the launch begins with a mix of both kinds.
+    s.n_first = s.n_early = 0;
+    int64_t n_sweeps = 0;
+    for (size_t i = 0; i < s.pieces.size(); i++) n_sweeps += (i == 0 || s.pieces[i].run != s.pieces[i - 1].run) * Hkv;
+    const int64_t units = (n_items + (waves >> s.waves_log2) - 1) / (waves >> s.waves_log2);
+    if (sweeps && n_items > 0 && n_sweeps + units > wg_slots) {
+        s.n_first = (int)std::min<int64_t>(n_sweeps, std::max<int64_t>(1, (int64_t)((double)wg_slots * share / Hkv + 0.5)) * Hkv);
+        s.n_early = (int)(std::min<int64_t>(units, std::max<int64_t>(wg_slots - s.n_first, 0)) / Hkv * Hkv);
+    }
 }
+
+// Tiles of the longest sequence that a sweep may cover.
+int64_t longest_chunk(const tc_plan *p) {
+    int64_t n = 0;
+    for (int q = 0; q < p->S; q++) n = std::max<int64_t>(n, p->ctx_len[q] + (p->q_start[q + 1] - p->q_start[q]));
+    return (n + kPrefillTileTokens - 1) / kPrefillTileTokens;
+}
+
+// Workgroups of four waves, several to a compute unit, where sweeps are short: one's start and end run beside another's tiles.
+int choose_sweep_waves(int64_t tiles) { return tiles <= kShortSweepTiles ? kSmallWaves : kMixedWaves; }
 
 bool fits(int64_t rows) { return rows < (int64_t)1 << 31; }
 
@@ -117,34 +185,38 @@ tc_status lay_out(const tc_plan *p, SpanList &s) {
     if (!fits(rows) || !fits(pieces * Hkv) || !fits(units * Hkv)) return fail(TC_ERR_SPAN, "the batch has more partial results than 2^31 rows");
     s.n_rows = rows;
 
-    // sweeps, the longest first
-    s.order.resize(s.blocks.size());
-    std::iota(s.order.begin(), s.order.end(), 0);
-    std::stable_sort(s.order.begin(), s.order.end(), [&](int x, int y) {
-        return (tiles_of(s.blocks[x].runs) + s.blocks[x].k - 1) / s.blocks[x].k > (tiles_of(s.blocks[y].runs) + s.blocks[y].k - 1) / s.blocks[y].k;
-    });
+    // Pieces in the order of their runs, whole blocks the longest first; the records of the runs' first pieces come first, those of the others behind them.
+    if (pieces == (int64_t)s.blocks.size())
+        std::stable_sort(s.pieces.begin(), s.pieces.end(), [](const SpanPiece &x, const SpanPiece &y) { return x.t1 - x.t0 > y.t1 - y.t0; });
+    int n_runs = 0;
+    for (size_t i = 0; i < s.pieces.size(); i++) n_runs += i == 0 || s.pieces[i].run != s.pieces[i - 1].run;
     s.records.assign((size_t)pieces * kRecordInts, 0);
-    int32_t *r = s.records.data();
-    for (const int i : s.order) {
-        const SpanBlock &b = s.blocks[i];
-        const int n = tiles_of(b.runs), n_pages = b.runs.pages();
+    int32_t first = 0, next = n_runs, *before = nullptr;
+    for (size_t i = 0; i < s.pieces.size(); i++) {
+        const SpanPiece &x = s.pieces[i];
+        const SpanBlock &b = s.blocks[x.block];
+        const bool begins = i == 0 || x.run != s.pieces[i - 1].run;
+        const int32_t index = begins ? first++ : next++;
+        if (!begins) before[SR_NEXT] = index;
+        int32_t *r = s.records.data() + (size_t)index * kRecordInts;
+        before = r;
         const int32_t *ids = p->host + p->off_pages + b.page_off;
-        for (int c = 0; c < b.k; c++, r += kRecordInts) {
-            r[RC_T0] = (int32_t)((int64_t)n * c / b.k);
-            r[RC_T1] = (int32_t)((int64_t)n * (c + 1) / b.k);
-            r[RC_REGION] = b.row0 < 0 ? -1 : (int32_t)(b.row0 + (int64_t)c * b.npos * G);
-            r[SR_KVROWS] = (int32_t)b.kv_rows;
-            r[RC_POS0] = 0;
-            r[RC_NPOS] = b.npos;
-            r[RC_QROW0] = b.qrow;
-            r[RC_CTX] = b.pos;
-            r[RC_PAGEOFF] = b.page_off;
-            r[SR_A] = b.runs.a; r[SR_H] = b.runs.h; r[SR_F] = b.runs.f; r[SR_B] = b.runs.b; r[SR_C] = b.runs.c; r[SR_E] = b.runs.e;
-            for (int x = 0; x < kRecordInts - RC_IDS; x++) r[RC_IDS + x] = ids[b.runs.page(std::min(r[RC_T0] * kTilePages + x, n_pages - 1))];
-        }
+        const int n_pages = b.runs.pages();
+        r[RC_T0] = x.t0;
+        r[RC_T1] = x.t1;
+        r[RC_REGION] = b.row0 < 0 ? -1 : (int32_t)(b.row0 + (int64_t)x.c * b.npos * G);
+        r[SR_KVROWS] = (int32_t)b.kv_rows;
+        r[SR_NEXT] = -1;
+        r[RC_POS0] = 0;
+        r[RC_NPOS] = b.npos;
+        r[RC_QROW0] = b.qrow;
+        r[RC_CTX] = b.pos;
+        r[RC_PAGEOFF] = b.page_off;
+        r[SR_A] = b.runs.a; r[SR_H] = b.runs.h; r[SR_F] = b.runs.f; r[SR_B] = b.runs.b; r[SR_C] = b.runs.c; r[SR_E] = b.runs.e;
+        for (int at = 0; at < kRecordInts - RC_IDS; at++) r[RC_IDS + at] = ids[b.runs.page(std::min(x.t0 * kTilePages + at, n_pages - 1))];
     }
     s.n_records = (int)pieces;
-    s.n_sweeps = (int)(pieces * Hkv);
+    s.n_sweeps = n_runs * Hkv;
 
     // decode items, the longest first, in whole workgroups
     s.order.resize(s.entries.size());
@@ -203,6 +275,7 @@ void add_merges(const tc_plan *p, SpanList &s) {
         int32_t m[kSpanItemInts] = {};
         m[SM_QROW] = row;
         m[SM_N] = end - row;
+        s.merge_rows = std::max(s.merge_rows, end - row);
         const auto put = [&](const SpanPart *x, int at) {
             if (!x) return;
             m[at] = (int32_t)(x->row0 + (int64_t)(row - x->qrow) * p->G);
@@ -218,17 +291,37 @@ void add_merges(const tc_plan *p, SpanList &s) {
     s.n_merge = (int)(s.merge.size() / kSpanItemInts);
 }
 
+// Decodes over a window, a workgroup to an item, and not too many of them: the last workgroup of a sequence and KV head to leave a partial result combines them.  (Where tokens are
+// shared the rows of a group would be combined by one workgroup, one after the other: 4 decodes behind 2048 shared tokens, 32/8 heads, 15 us, with a second launch 11.)
+void fuse(const tc_plan *p, SpanList &s) {
+    s.fused = s.blocks.empty() && s.first.empty() && s.n_merge > 0 && s.items_per_wg() == 1 && (int64_t)s.n_merge * p->Hkv <= kCounterInts && s.n_rows * p->D * 4 < (int64_t)1 << 31;
+    if (!s.fused) return;
+    s.counter_stride = kCounterLine;
+    while ((int64_t)s.n_merge * p->Hkv * s.counter_stride > kCounterInts) s.counter_stride /= 2;
+    s.order.assign((size_t)p->T, -1);  // the merge item of each row
+    for (int m = 0; m < s.n_merge; m++) s.order[s.merge[(size_t)m * kSpanItemInts + SM_QROW]] = m;
+    for (size_t i = 0; i < s.items.size(); i += kSpanItemInts) {
+        int32_t *d = s.items.data() + i;
+        if (d[SD_ROW] < 0) continue;
+        d[SD_MERGE] = s.order[d[SD_QROW]];
+        d[SD_PARTS] = s.merge[(size_t)d[SD_MERGE] * kSpanItemInts + SM_NB];
+    }
+}
+
 void clear(SpanList &s) {
     s.ready = false;
     s.blocks.clear();
     s.entries.clear();
+    s.pieces.clear();
     s.first.clear();
     s.second.clear();
     s.merge.clear();
     s.n_records = s.n_sweeps = s.n_items = s.n_merge = 0;
     s.waves_log2 = 0;
-    s.max_cols = 1;
-    s.wide = false;
+    s.max_cols = s.merge_rows = 1;
+    s.wide = s.fused = false;
+    s.n_first = s.n_early = 0;
+    s.sweep_waves = kMixedWaves;
     s.n_rows = 0;
     s.build_ns = s.upload_ns = 0;
 }
@@ -242,10 +335,12 @@ tc_status finish(tc_plan *p, SpanList &s, size_t n_first_blocks, size_t n_first_
     for (size_t i = 0; i < s.entries.size(); i++)
         if (s.entries[i].row0 >= 0) (i < n_first_entries ? s.first : s.second).push_back(part_of(p, s.entries[i]));
     add_merges(p, s);
+    fuse(p, s);
     s.off_records = 0;
     s.off_items = s.records.size();
     s.off_merge = s.off_items + s.items.size();
-    const size_t total = std::max<size_t>(s.off_merge + s.merge.size(), 1);
+    s.off_counters = (s.off_merge + s.merge.size() + kCounterLine - 1) / kCounterLine * kCounterLine;
+    const size_t n_counters = s.fused ? (size_t)s.n_merge * p->Hkv * s.counter_stride : 0, total = std::max<size_t>(s.off_counters + n_counters, 1);
     s.on_device = p->on_device;
     if (int err = begin_plan_host(&s, total)) {
         set_error(std::string("host buffer of the work list: ") + hip_error_text(err));
@@ -254,6 +349,7 @@ tc_status finish(tc_plan *p, SpanList &s, size_t n_first_blocks, size_t n_first_
     std::memcpy(s.host + s.off_records, s.records.data(), s.records.size() * sizeof(int32_t));
     std::memcpy(s.host + s.off_items, s.items.data(), s.items.size() * sizeof(int32_t));
     std::memcpy(s.host + s.off_merge, s.merge.data(), s.merge.size() * sizeof(int32_t));
+    std::memset(s.host + s.off_counters, 0, n_counters * sizeof(int32_t));
     s.host_n = total;
     const auto t1 = std::chrono::steady_clock::now();
     s.build_ns = std::chrono::duration_cast<std::chrono::nanoseconds>(t1 - t0).count();
@@ -301,6 +397,8 @@ tc_status tc_plan_set_window(tc_plan *p, int32_t window, int32_t sinks, void *st
         if (window < 1 || sinks < 0) return fail(TC_ERR_ARG, "window must be at least 1 and sinks at least 0");
         s.window = window;
         s.sinks = sinks;
+        // (the tiles of a block of 256 rows in the middle of a long sequence)
+        s.sweep_waves = choose_sweep_waves(std::min<int64_t>(((int64_t)window + sinks) / kPrefillTileTokens + 2, longest_chunk(p)));
         for (int q = 0; q < p->S; q++) add_sequence(p, s, q, 0);
         return finish(p, s, 0, 0, stream, t0);
     });
@@ -330,23 +428,37 @@ tc_status tc_plan_set_shared(tc_plan *p, int32_t num_groups, const int32_t *seq_
         }
         s.window = INT32_MAX;
         s.sinks = 0;
-        // what is shared: a group's rows as one matrix, over the tokens before all of them
+        s.sweep_waves = choose_sweep_waves(longest_chunk(p));
+        // What is shared: the rows of a group's sequences as one matrix, over the tokens before all of them.  A chunk that fills a block of rows by itself has its own sweep over
+        // everything, which reads what is shared once for the block as well and leaves nothing to combine; the sequences between such chunks are taken together.
+        const auto alone = [&](int q) { return (p->q_start[q + 1] - p->q_start[q]) * p->G >= kPrefillRows; };
+        const auto together = [&](int q, int q1) {  // end of the run of sequences from q on that are taken together
+            while (q < q1 && !alone(q)) q++;
+            return q;
+        };
         for (int g = 0; g < num_groups; g++) {
-            const int q0 = seq_start[g], q1 = seq_start[g + 1], pages = prefix_len[g] / kBlock;
-            if (pages == 0 || q1 - q0 == 1) continue;
-            const int row0 = p->q_start[q0], rows = p->q_start[q1] - row0, after = 1 << 30;
-            const SpanRuns all = {pages, 0, 0, 0, 0, 0};
-            if (rows * p->G <= 16) {
-                s.entries.push_back({row0, rows * p->G, after, p->page_off[q0], all, true});
-                continue;
+            const int q1 = seq_start[g + 1], pages = prefix_len[g] / kBlock;
+            for (int q = seq_start[g], end; q < q1 && pages > 0; q = std::max(end, q + 1)) {
+                end = together(q, q1);
+                if (end - q < 2) continue;
+                const int row0 = p->q_start[q], rows = p->q_start[end] - row0, after = 1 << 30;
+                const SpanRuns all = {pages, 0, 0, 0, 0, 0};
+                if (rows * p->G <= 16) {
+                    s.entries.push_back({row0, rows * p->G, after, p->page_off[q], all, true});
+                    continue;
+                }
+                const int per = s.rows_per_block() / p->G;
+                for (int i = 0; i < rows; i += per) s.blocks.push_back({row0 + i, std::min(per, rows - i), after, p->page_off[q], all, true});
             }
-            const int per = kPrefillRows / p->G;
-            for (int i = 0; i < rows; i += per) s.blocks.push_back({row0 + i, std::min(per, rows - i), after, p->page_off[q0], all, true});
         }
         const size_t n_blocks = s.blocks.size(), n_entries = s.entries.size();
         for (int g = 0; g < num_groups; g++) {
-            const int q0 = seq_start[g], q1 = seq_start[g + 1];
-            for (int q = q0; q < q1; q++) add_sequence(p, s, q, q1 - q0 > 1 ? prefix_len[g] / kBlock : 0);
+            const int q1 = seq_start[g + 1];
+            for (int q = seq_start[g]; q < q1;) {
+                const int end = std::max(together(q, q1), q + 1);
+                const int from = end - q < 2 ? 0 : prefix_len[g] / kBlock;
+                for (; q < end; q++) add_sequence(p, s, q, from);
+            }
         }
         return finish(p, s, n_blocks, n_entries, stream, t0);
     });
@@ -361,8 +473,10 @@ tc_status tc_plan_get_span_info(const tc_plan *p, int32_t shared, tc_span_info *
     std::memset(info, 0, sizeof *info);
     info->ready = s.ready;
     info->num_sweeps = s.n_records;
+    info->num_sweep_workgroups = s.n_sweeps;
     info->num_decode_items = s.n_items;
     info->num_merge_items = s.n_merge;
+    info->merge_launch = s.n_merge > 0 && !s.fused;
     info->waves_per_item = 1 << s.waves_log2;
     info->grid_blocks = s.ready ? s.grid_blocks() : 0;
     info->block_threads = 64 * s.waves();

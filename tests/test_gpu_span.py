@@ -270,13 +270,24 @@ def test_blocks_outside_the_window_may_belong_to_anyone(tc):
     assert (table == free).sum() > 20 and torch.isnan(d.k_pool.view(torch.bfloat16)).any()
 
 
+GRAPHS = {  # q_len, ctx, groups, window: partial results combined by a second launch, by the last workgroup to leave one, or none
+    "chunk": ([1] * 20 + [33], [1024 + 9 * i for i in range(21)], [(21, 1024)], 900),
+    "decodes": ([1] * 3, [4096, 5000, 4111], [(3, 4096)], 4000),
+    "short": ([1] * 3, [64, 80, 100], [(3, 64)], 50),
+}
+
+
 @pytest.mark.parametrize("shared", [False, True])
-def test_graphs_streams_and_workspaces(tc, shared):
-    """Captured and replayed with eager work between, on another stream, and two calls of one plan at a time on workspaces of their own: the same bits every time."""
+@pytest.mark.parametrize("name", list(GRAPHS))
+def test_graphs_streams_and_workspaces(tc, name, shared):
+    """Captured and replayed with eager work between, on another stream, and two plans at a time on workspaces of their own: the same bits every time."""
     import torch
-    c = Case(8, 2, 128, [1] * 20 + [33], [1024 + 9 * i for i in range(21)], "bf16", [(21, 1024)])
+    q_len, ctx, groups, window = GRAPHS[name]
+    c = Case(8, 2, 128, q_len, ctx, "bf16", groups)
     d = Device(tc, c)
-    d.set() if shared else d.set(900, 4)
+    d.set() if shared else d.set(window, 4)
+    info = d.plan.span_info(shared)
+    assert (info.num_merge_items > 0, info.merge_launch) == {"chunk": (True, 1), "decodes": (True, int(shared)), "short": (shared, int(shared))}[name]
     d.run()
     want = d.outputs()
     g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
@@ -290,16 +301,15 @@ def test_graphs_streams_and_workspaces(tc, shared):
         d.run()
         assert np.array_equal(d.outputs(), want)
     streams = [torch.cuda.Stream() for _ in range(2)]
-    first = d.workspace
-    both = [(torch.full_like(d.out, -1), torch.empty_like(first), st) for st in streams]
+    both = [Device(tc, c) for _ in streams]
+    for x in both:
+        x.set() if shared else x.set(window, 4)
     torch.cuda.synchronize()
     for _ in range(5):
-        for out, ws, st in both:
-            d.workspace = ws
-            d.run(out=out, stream=st)
-    torch.cuda.synchronize()
-    for out, _, _ in both:
-        assert np.array_equal(out[:-1].cpu().numpy().view(np.uint16), want)
+        for x, st in zip(both, streams):
+            x.run(stream=st)
+    for x in both:
+        assert np.array_equal(x.outputs(), want)
 
 
 def test_lists_are_made_anew(tc):

@@ -104,8 +104,18 @@ def check(plan, Hq, Hkv, q_start, ctx, table, window, sinks, shared=False):
                         at = base + h * kv + i * step + x
                         assert rows[at] == t * Hq + head
                         used[at] += 1
+    if info.num_merge_items and not info.merge_launch:  # every partial result is waited for by the last of its group
+        assert not shared and len(records) == 0 and info.waves_per_item * 64 == info.block_threads
+        parts = np.zeros((len(merge), Hkv), np.int32)
+        for d in items[items[:, 5] >= 0]:
+            assert merge[d[14]][0] == d[4] and merge[d[14]][1] == 1 and d[7] == G and d[15] == merge[d[14]][8]
+            parts[d[14], d[1]] += 1
+        assert (parts == merge[:, 8:9]).all()
     assert (used == 1).all() and ((direct > 0) ^ (merged > 0)).all() and (direct + merged == 1).all()
-    assert info.grid_blocks == info.num_sweeps * Hkv + len(items) * info.waves_per_item // (info.block_threads // 64)
+    chained = [r[15] for r in records if r[15] >= 0]  # every record is one workgroup's, the first of them or behind another
+    runs = info.num_sweep_workgroups // Hkv
+    assert sorted(list(range(runs)) + chained) == list(range(len(records))) and runs * Hkv == info.num_sweep_workgroups
+    assert info.grid_blocks == info.num_sweep_workgroups + len(items) * info.waves_per_item // (info.block_threads // 64)
     return info
 
 
@@ -171,7 +181,8 @@ def test_shared_tokens_are_read_once_for_the_group(tc):  # noqa: F811
     plan = tc.Plan(tc.make_pool(32, 8, 128, blocks), q_start, ctx, table, host_only=True)
     plan.set_shared([0, 64], [1024])
     records = plan.span_items(0, True)
-    assert (records[:, 1] - records[:, 0]).sum() == 1024 // 64 and (records[:, 9] == 64).all()  # 64 rows of four heads are one sweep's 256 pairs
+    blocks = 256 // (32 * plan.span_info(True).block_threads // 64)  # 64 rows of four heads are 256 pairs: a sweep or two
+    assert (records[:, 1] - records[:, 0]).sum() == blocks * 1024 // 64 and (records[:, 9] == 64 // blocks).all()
     items = plan.span_items(1, True)
     assert (items[:, 3] - items[:, 2]).sum() == 64 * 8 * 2
 
@@ -257,4 +268,4 @@ def test_an_empty_batch_is_a_no_op(tc):  # noqa: F811
     plan.set_shared([0], [])
     for call in (tc.tc_window_attention, tc.tc_shared_attention):
         call(plan, pool, None, None, 0.0)
-    assert plan.window_workspace_bytes == plan.shared_workspace_bytes == 0 and C.sizeof(tc.tc_span_info) == 56
+    assert plan.window_workspace_bytes == plan.shared_workspace_bytes == 0 and C.sizeof(tc.tc_span_info) == 64
