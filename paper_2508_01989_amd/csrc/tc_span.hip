@@ -89,7 +89,7 @@ __device__ __forceinline__ void span_decode_sweep(const AttnArgs &A, int kvh, in
 
 // Vectors of four elements v0, v0 + step, .. of the output rows of a merge item, for KV head h: each from its row's partial results, i of them in workspace row
 // base + h * kv + i * step + r for row r of the item, for either of two lists.  PEER: other compute units have stored them while this kernel runs.
-constexpr int kSpanMergeThreads = 256, kSpanMergeBatch = 4;
+constexpr int kSpanMergeThreads = 256, kSpanMergeBatch = 8;
 template <int D, class E, bool PEER>
 __device__ __forceinline__ void span_merge_rows(const int32_t *it, int h, const float *ws, uint16_t *out, int64_t n_rows, int Hq, int G, int v0, int v_step) {
     constexpr int VR = D / 4;

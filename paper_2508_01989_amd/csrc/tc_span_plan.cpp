@@ -18,7 +18,8 @@ tc_status fail(tc_status s, const char *msg) {
 
 constexpr int kTilePages = kPrefillTileTokens / kBlock;
 constexpr int kMinSweepTiles = 4;   // a piece of a cut sweep is not shorter than this
-constexpr double kPieceUs = 6, kMergeUs = 8;  // what a piece costs on top of its tiles: its start and end; and the launch that combines pieces
+constexpr double kAloneSmall = 0.6;  // a tile of a workgroup of four waves that has its compute unit to itself, to one of eight's
+constexpr double kPieceUs = 8, kMergeUs = 8;  // what a piece costs on top of its tiles: its start and end; and the launch that combines pieces
 constexpr int kUncutPages = 28, kFewUncutPages = 10;   // a wave gets up to that many before an item is cut: where uncut items fill the chip, where they do not
 constexpr int kShortSweepTiles = 32;
 constexpr int kMinWavePages = 6;    // nor does a wave get fewer pages of a decode item that is shared out
@@ -106,19 +107,19 @@ void share_out(const tc_plan *p, SpanList &s) {
     const bool sweeps = !s.blocks.empty();
     const int waves = s.blocks.empty() ? kDecodeWaves : s.sweep_waves;
     const int64_t wg_slots = sweeps ? (int64_t)kNumCu * (s.sweep_waves == kMixedWaves ? 1 : small_wg_per_cu(p->D)) : kNumCu * kDecodeWgPerCu;
-    const double tile_us = kSweepTileUs * p->D / 128 * s.sweep_waves / kMixedWaves;  // of a workgroup, per compute unit
+    const double tile_us = kSweepTileUs * p->D / 128 * s.sweep_waves / kMixedWaves;  // of a workgroup's share of its compute unit
     const double sweep_us = ((double)tiles * tile_us + (double)s.blocks.size() * kPieceUs) * Hkv;
     const double bytes = (double)pages * Hkv * kBlock * p->token_bytes(), stream_us = bytes / kStreamCuBytesPerUs;
     const double share = sweep_us / std::max(1e-9, sweep_us + stream_us);  // of the compute units that sweep
     if (sweeps) {
         const int64_t whole = (int64_t)s.blocks.size() * Hkv;
-        const int64_t target = std::max<int64_t>(Hkv, (int64_t)((double)wg_slots * (pages > 0 ? share : 1.0)));  // workgroups that sweep at a time
+        const int64_t target = std::max<int64_t>(Hkv, (int64_t)((double)kNumCu * (pages > 0 ? share : 1.0)));  // compute units that sweep at a time
         const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(target / Hkv, tiles / kMinSweepTiles));
-        // Few blocks: whole, or in level runs, which pay a start and an end for each piece and a launch that combines them.  Not beside a stream that takes longer than the longest sweep.
-        const double per_tile = tile_us * (double)wg_slots / kNumCu, piece = kPieceUs;
-        const double t_whole = std::max((double)longest * per_tile + piece, bytes / kStreamBytesPerUs);
-        const double t_level = ((double)tiles * per_tile + (double)(s.blocks.size() + bins - 1) * piece) / (double)bins + kMergeUs;
-        if (whole < target && std::max(t_level, bytes / kStreamBytesPerUs) < 0.95 * t_whole) level(s, (int)bins, piece / per_tile);
+        // Fewer blocks than units: whole, or in level runs, which pay a start and an end for each piece and a launch that combines them.  Not beside a stream that takes longer than the longest sweep.
+        const double alone_us = kSweepTileUs * p->D / 128 * (s.sweep_waves == kMixedWaves ? 1.0 : kAloneSmall);
+        const double t_whole = std::max((double)longest * alone_us + kPieceUs, bytes / kStreamBytesPerUs);
+        const double t_level = ((double)tiles * alone_us + (double)(s.blocks.size() + bins - 1) * kPieceUs) / (double)bins + kMergeUs;
+        if (whole < target && std::max(t_level, bytes / kStreamBytesPerUs) < 0.95 * t_whole) level(s, (int)bins, kPieceUs / alone_us);
     }
     if (s.pieces.empty())
         for (size_t i = 0; i < s.blocks.size(); i++) s.pieces.push_back({(int32_t)i, 0, tiles_of(s.blocks[i].runs), 0, (int32_t)i});
@@ -158,8 +159,11 @@ int64_t longest_chunk(const tc_plan *p) {
     return (n + kPrefillTileTokens - 1) / kPrefillTileTokens;
 }
 
-// Workgroups of four waves, several to a compute unit, where sweeps are short: one's start and end run beside another's tiles.
-int choose_sweep_waves(int64_t tiles) { return tiles <= kShortSweepTiles ? kSmallWaves : kMixedWaves; }
+// Workgroups of four waves, several to a compute unit, where sweeps are short: one's start and end run beside another's tiles, or a sweep beside decodes.  (us, four waves / eight.
+// Windows: 64/8 heads, head_dim 128, 8192 tokens, of 512 213 / 235, 1024 328 / 325, 2048 556 / 538, 5000 1213 / 1144; 32/8, 2000 with 60 decodes, 512 47 / 53, 2048 112 / 132, 5000
+// 222 / 236; 500 with 60 decodes, 512 28 / 42, 2048 81 / 94, 5000 135 / 125; head_dim 64, 64/8, 8192, 512 109 / 137, 2048 314 / 338, 5000 701 / 697.  Shared tokens:
+// 300 decodes behind 1024, 32/8, 76 / 83, 64 behind 2048 26 / 26, 128 behind 8192 65 / 51; head_dim 64, 16/2, 128 behind 8192 22 / 25, 100 behind 16384 24 / 28.)
+int choose_sweep_waves(int64_t tiles, int64_t short_tiles) { return tiles <= short_tiles ? kSmallWaves : kMixedWaves; }
 
 bool fits(int64_t rows) { return rows < (int64_t)1 << 31; }
 
@@ -398,7 +402,7 @@ tc_status tc_plan_set_window(tc_plan *p, int32_t window, int32_t sinks, void *st
         s.window = window;
         s.sinks = sinks;
         // (the tiles of a block of 256 rows in the middle of a long sequence)
-        s.sweep_waves = choose_sweep_waves(std::min<int64_t>(((int64_t)window + sinks) / kPrefillTileTokens + 2, longest_chunk(p)));
+        s.sweep_waves = choose_sweep_waves(std::min<int64_t>(((int64_t)window + sinks) / kPrefillTileTokens + 2, longest_chunk(p)), (p->D == 64 || p->n_decode_seqs > 0 ? 2 : 1) * kShortSweepTiles);
         for (int q = 0; q < p->S; q++) add_sequence(p, s, q, 0);
         return finish(p, s, 0, 0, stream, t0);
     });
@@ -428,7 +432,7 @@ tc_status tc_plan_set_shared(tc_plan *p, int32_t num_groups, const int32_t *seq_
         }
         s.window = INT32_MAX;
         s.sinks = 0;
-        s.sweep_waves = choose_sweep_waves(longest_chunk(p));
+        s.sweep_waves = choose_sweep_waves(longest_chunk(p), p->D == 64 ? INT64_MAX : kShortSweepTiles);
         // What is shared: the rows of a group's sequences as one matrix, over the tokens before all of them.  A chunk that fills a block of rows by itself has its own sweep over
         // everything, which reads what is shared once for the block as well and leaves nothing to combine; the sequences between such chunks are taken together.
         const auto alone = [&](int q) { return (p->q_start[q + 1] - p->q_start[q]) * p->G >= kPrefillRows; };

@@ -174,6 +174,16 @@ def test_long_chunks(tc, heads, D, dtype):
         check(d, window, sinks, some=12)
 
 
+@pytest.mark.parametrize("D, dtype, window, sinks", [(128, "bf16", 2100, 5), (64, "fp16", 2301, 0), (128, "fp16", 40000, 0)])
+def test_more_blocks_than_workgroups_at_a_time(tc, D, dtype, window, sinks):
+    """Whole blocks of rows, of which the first of a sequence have one tile and the last ones dozens."""
+    d = check(Device(tc, Case(32, 2, D, [2600, 2203], [0, 2100], dtype)), window, sinks, some=40)
+    first = d.outputs()
+    d.out.fill_(-1)
+    d.run()
+    assert np.array_equal(d.outputs(), first)
+
+
 def test_a_window_past_every_token_is_mixed_attention(tc):
     import torch
     c = Case(8, 2, 128, *MIXED)
