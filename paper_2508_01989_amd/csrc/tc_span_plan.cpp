@@ -19,7 +19,7 @@ tc_status fail(tc_status s, const char *msg) {
 constexpr int kTilePages = kPrefillTileTokens / kBlock;
 constexpr int kMinSweepTiles = 4;   // a piece of a cut sweep is not shorter than this
 constexpr double kAloneSmall = 0.6;  // a tile of a workgroup of four waves that has its compute unit to itself, to one of eight's
-constexpr double kPieceUs = 8, kMergeUs = 8;  // what a piece costs on top of its tiles: its start and end; and the launch that combines pieces
+constexpr double kPieceUs = 8, kMergeUs = 8, kPartUs = 0.15;  // what a piece costs on top of its tiles: its start and end; the launch that combines pieces, and what each piece of a row adds to it
 constexpr int kUncutPages = 28, kFewUncutPages = 10;   // a wave gets up to that many before an item is cut: where uncut items fill the chip, where they do not
 constexpr int kShortSweepTiles = 32;
 constexpr int kMinWavePages = 6;    // nor does a wave get fewer pages of a decode item that is shared out
@@ -114,18 +114,28 @@ void share_out(const tc_plan *p, SpanList &s) {
     if (sweeps) {
         const int64_t whole = (int64_t)s.blocks.size() * Hkv;
         const int64_t target = std::max<int64_t>(Hkv, (int64_t)((double)kNumCu * (pages > 0 ? share : 1.0)));  // compute units that sweep at a time
-        const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(target / Hkv, tiles / kMinSweepTiles));
-        // Fewer blocks than units: whole, or in level runs, which pay a start and an end for each piece and a launch that combines them.  Not beside a stream that takes longer than the longest sweep.
-        const double alone_us = kSweepTileUs * p->D / 128 * (s.sweep_waves == kMixedWaves ? 1.0 : kAloneSmall);
-        const double t_whole = std::max((double)longest * alone_us + kPieceUs, bytes / kStreamBytesPerUs);
-        const double t_level = ((double)tiles * alone_us + (double)(s.blocks.size() + bins - 1) * kPieceUs) / (double)bins + kMergeUs;
-        if (whole < target && std::max(t_level, bytes / kStreamBytesPerUs) < 0.95 * t_whole) level(s, (int)bins, kPieceUs / alone_us);
+        // Fewer blocks than units: whole, or in level runs, which pay a start and an end for each piece and a launch that combines them; one run to a unit, or as many as it holds where the
+        // tiles are many.  Not beside a stream that takes longer than the longest sweep.  (us, one / as many as fit, head_dim 64: 97 tokens behind 4769, 32/8 heads, 20 / 28; 19 decodes
+        // behind 15264, 32/8, 20 / 25; 234 tokens and 17 decodes behind 9280, 32/32, 88 / 47; 249 decodes behind 6704, 64/8, 66 / 54.)
+        const double alone_us = kSweepTileUs * p->D / 128 * (s.sweep_waves == kMixedWaves ? 1.0 : kAloneSmall), all_us = bytes / kStreamBytesPerUs;
+        double best = 0.95 * std::max((double)longest * alone_us + kPieceUs, all_us);
+        double piece_tiles = 0;
+        int64_t bins = 0;
+        for (int64_t r = 1, per_cu = wg_slots / kNumCu; whole < target && r <= per_cu; r++) {
+            const int64_t n = std::max<int64_t>(1, std::min<int64_t>(target * r / Hkv, tiles / kMinSweepTiles));
+            const double run_us = std::max(alone_us, tile_us * std::max(1.0, (double)(n * Hkv) / kNumCu));  // a tile of a run beside the others of its unit
+            const double parts = (double)longest * (double)n / (double)tiles;
+            const double t = std::max(((double)tiles * run_us + (double)((int64_t)s.blocks.size() + n - 1) * kPieceUs) / (double)n + kMergeUs + kPartUs * parts, all_us);
+            if (t < best) best = t, bins = n, piece_tiles = kPieceUs / run_us;
+        }
+        if (bins > 0) level(s, (int)bins, piece_tiles);
     }
     if (s.pieces.empty())
         for (size_t i = 0; i < s.blocks.size(); i++) s.pieces.push_back({(int32_t)i, 0, tiles_of(s.blocks[i].runs), 0, (int32_t)i});
 
     // Pages of a wave: as many as keep all waves that the chip holds busy, but no fewer than are worth a wave.
-    const int64_t slots = wg_slots * waves, least = kMinWavePages;
+    // (Beside sweeps half as many: finer units for the units that sweeps leave free.)
+    const int64_t slots = wg_slots * waves * (sweeps ? 2 : 1), least = kMinWavePages;
     const int64_t per_wave = std::min<int64_t>(kMaxSplitPages, std::max<int64_t>(least, (pages * Hkv + slots - 1) / slots));
     s.waves_log2 = 0;
     if (!s.entries.empty()) {
