@@ -494,7 +494,8 @@ __device__ __forceinline__ int page_id_read(const char *slot, int lane) {
 }
 
 // A barrier behind this wave's LDS accesses that leaves its direct-to-LDS loads in flight (those have waits of their own).  Where a wave also
-// stores to LDS the compiler puts a wait for all of them before the barrier of __syncthreads.
+// stores to LDS the compiler puts a wait for all of them before the barrier of __syncthreads; and at the top of a loop it may leave out the wait for the LDS
+// accesses of the round before (workgroups of four waves had reads of operands, and the stores of a fixed V, in flight across the barrier of a step).
 __device__ __forceinline__ void barrier_lds() {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -1172,8 +1173,7 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         // have both operand addresses in registers here, outside the scheduled regions below
         asm volatile("" : "+v"(k_nxt), "+v"(v_cur));
         // every wave is done with step j - 1; the copies waited for at its end (a cache in 8 bits: the tile widened in it) are visible
-        if constexpr (KVQ) barrier_lds();
-        else __syncthreads();
+        barrier_lds();
         if (NEXT && copier) copies(j);  // past the end of the range the copies are never read
         const std::true_type yes;
         const auto phases = [&] {
@@ -1207,8 +1207,7 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
             wait_loads_but<TileWidener<D, E>::kLoads>();
         } else if (copier) wait_loads_but<(NS + VS - 4) * C::kRuns>();
         for (int j = 0; j < n_sweep; j++) {
-            if constexpr (KVQ) barrier_lds();
-            else __syncthreads();
+            barrier_lds();
             if (copier && j + 1 < n_sweep) {
                 copies(j);
                 if constexpr (KVQ) {
