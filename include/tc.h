@@ -299,7 +299,7 @@ typedef struct {
     const int32_t *positions;              /* DEVICE [T] positions of the rows, or NULL: those of the plan (ctx_len[s] + i)             */
 } tc_qkv_rows;
 
-/* q_out DEVICE [T][Hq][D], k_out DEVICE [T][Hkv][D]; v is not used.  Rows that are packed already may be their own output (q_out = q, k_out = k).
+/* q_out DEVICE [T][Hq][D], k_out DEVICE [T][Hkv][D]; v is not used.  Rows that are packed already may be their own output (q_out = q, k_out = k; TC_ERR_ARG if they are not packed).
  * Serves plans of either kind of cache: k_out and v are what the appends of both take.
  * q, k, v, the weights and the outputs are 16-byte aligned (TC_ERR_ARG), and the current device is the plan's (TC_ERR_DEVICE). */
 tc_status tc_qk_norm_rotate(const tc_plan *plan, const tc_qkv_rows *rows, void *q_out, void *k_out, void *stream);
@@ -355,7 +355,7 @@ tc_status tc_plan_get_span_info(const tc_plan *plan, int32_t shared, tc_span_inf
 /* Copy them to HOST memory.  kind 0: sweeps, 32 int32 each; 1: decode items, 16 each; 2: merge items, 16 each.  The pages of a sweep or decode item are places in a list that
  * is made of runs of pages of a sequence: [0, a), [b, c), then page a if h, [f, b), [c, e).
  *   sweep  {first 64-token tile of the list, end tile, a, h, first workspace row of KV head 0 (-1 = writes out), f, rows to the next KV head, b, 0, packed rows, first packed row,
- *           position of the first row (2^30: behind all tokens), start of the sequence's pages, c, e, the workgroup's next record or -1, pool blocks of the first 16 places}
+ *           position of the first row (2^31 - 1024: behind all tokens), start of the sequence's pages, c, e, the workgroup's next record or -1, pool blocks of the first 16 places}
  *   decode {position, kv_head, first place, end place (the same: padding), first packed row, first workspace row (-1 = writes out), start of the sequence's pages,
  *           (row, head) pairs, a, h, f, b, c, e, then where there is no second launch the merge item and its partial results}
  *   merge  {first packed row, packed rows, then of two lists of partial results: workspace row of the first row and KV head 0, rows to the next KV head, partial results, rows

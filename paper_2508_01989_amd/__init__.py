@@ -168,10 +168,12 @@ def _row_stride(x):
     """Elements from a token's heads to the next token's in a tensor [T][heads][D]; 0 for None or an address."""
     if x is None or isinstance(x, int):
         return 0
-    strides = x.stride()
-    if len(strides) == 3 and (strides[1] != x.shape[2] or strides[2] != 1) and (strides[2] != 1 or x.shape[1] > 1):
-        raise ValueError("a token's heads must be adjacent")
-    return strides[0]
+    strides, token = x.stride(), 1
+    for n, stride in zip(reversed(x.shape[1:]), reversed(strides[1:])):
+        if n > 1 and stride != token:
+            raise ValueError("a token's heads must be adjacent")
+        token *= n
+    return strides[0] if x.shape[0] > 1 else token
 
 
 def make_qkv_rows(q, k, v=None, q_weight=None, k_weight=None, eps=1e-6, freq=None, rotary_dim=None, adjacent=False, positions=None,
@@ -179,6 +181,9 @@ def make_qkv_rows(q, k, v=None, q_weight=None, k_weight=None, eps=1e-6, freq=Non
     """Rows for tc_qk_norm_rotate: tensors [T][heads][D] whose heads are adjacent; a stride that is not given is the tensor's own.  rotary_dim: twice the length of freq unless given."""
     if rotary_dim is None:
         rotary_dim = 0 if freq is None else 2 * freq.numel()
+    for x, size, what in ((freq, 8, "freq is in 64-bit floating point"), (positions, 4, "positions are in 32 bits")):
+        if hasattr(x, "element_size") and x.element_size() != size:
+            raise ValueError(what)
     return tc_qkv_rows(_ptr(q), _ptr(k), _ptr(v), _row_stride(q) if q_stride is None else q_stride, _row_stride(k) if k_stride is None else k_stride,
                        _row_stride(v) if v_stride is None else v_stride, _ptr(q_weight), _ptr(k_weight), eps, rotary_dim, _ptr(freq), adjacent, _ptr(positions))
 
@@ -228,8 +233,9 @@ class Plan:
             self._refresh()
 
     def set_window(self, window, sinks=0, stream=None):
-        """tc_plan_set_window: this batch's work list for tc_window_attention."""
-        _check(lib().tc_plan_set_window(self.handle, int(window), int(sinks), _stream(stream)))
+        """tc_plan_set_window: this batch's work list for tc_window_attention.  More than 2^31 - 1 is all tokens."""
+        window, sinks = (max(-1, min(int(n), (1 << 31) - 1)) for n in (window, sinks))
+        _check(lib().tc_plan_set_window(self.handle, window, sinks, _stream(stream)))
 
     def set_shared(self, seq_start, prefix_len, stream=None):
         """tc_plan_set_shared: this batch's work list for tc_shared_attention; group g is sequences seq_start[g] .. seq_start[g + 1] - 1."""

@@ -275,6 +275,12 @@ tc_status tc_kvq_mixed_attention_append(const tc_plan *plan, const tc_kvq_pool *
 
 namespace {
 
+// Rows that are their own output lie as it does: a token would be written over the heads of another that are yet to be read.
+tc_status check_own_output(const tc_plan *plan, const void *in, const void *out, int64_t stride, int heads) {
+    if (in == out && plan->T > 1 && stride != (int64_t)heads * plan->D) return fail(TC_ERR_ARG, "rows that are their own output must be packed");
+    return TC_OK;
+}
+
 tc_status check_rows(const tc_plan *plan, const tc_qkv_rows *rows, bool needs_v) {
     if (rows->rotary_dim < 0 || rows->rotary_dim > plan->D || rows->rotary_dim % 8)
         return fail(TC_ERR_SHAPE, "rotary_dim must be a multiple of 8 from 0 to head_dim");
@@ -303,6 +309,7 @@ tc_status tc_qk_norm_rotate(const tc_plan *plan, const tc_qkv_rows *rows, void *
     if (st != TC_OK) return st;
     if (!q_out || !k_out) return fail(TC_ERR_NULL, "q_out or k_out is NULL");
     if (misaligned(q_out, 16) || misaligned(k_out, 16)) return fail(TC_ERR_ARG, "q_out and k_out must be 16-byte aligned");
+    if ((st = check_own_output(plan, rows->q, q_out, rows->q_stride, plan->Hq)) != TC_OK || (st = check_own_output(plan, rows->k, k_out, rows->k_stride, plan->Hkv)) != TC_OK) return st;
     if ((st = check_plan_device(plan)) != TC_OK) return st;
     return device_result(tc::launch_rows(plan, nullptr, rows, q_out, k_out, stream), "tc_qk_norm_rotate launch");
 }
@@ -314,6 +321,7 @@ tc_status tc_qk_norm_rotate_append(const tc_plan *plan, const tc_kv_pool *pool, 
     if ((st = check_rows(plan, rows, true)) != TC_OK) return st;
     if (!q_out) return fail(TC_ERR_NULL, "q_out is NULL");
     if (misaligned(q_out, 16)) return fail(TC_ERR_ARG, "q_out must be 16-byte aligned");
+    if ((st = check_own_output(plan, rows->q, q_out, rows->q_stride, plan->Hq)) != TC_OK) return st;
     if (misaligned(pool->k_pool, 16) || misaligned(pool->v_pool, 16)) return fail(TC_ERR_ARG, "k_pool and v_pool must be 16-byte aligned");
     if ((st = check_plan_device(plan)) != TC_OK) return st;
     return device_result(tc::launch_rows(plan, pool, rows, q_out, nullptr, stream), "tc_qk_norm_rotate_append launch");

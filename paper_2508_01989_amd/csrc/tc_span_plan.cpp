@@ -445,7 +445,7 @@ tc_status tc_plan_set_shared(tc_plan *p, int32_t num_groups, const int32_t *seq_
         s.sweep_waves = choose_sweep_waves(longest_chunk(p), p->D == 64 ? INT64_MAX : kShortSweepTiles);
         // What is shared: the rows of a group's sequences as one matrix, over the tokens before all of them.  A chunk that fills a block of rows by itself has its own sweep over
         // everything, which reads what is shared once for the block as well and leaves nothing to combine; the sequences between such chunks are taken together.
-        const auto alone = [&](int q) { return (p->q_start[q + 1] - p->q_start[q]) * p->G >= kPrefillRows; };
+        const auto alone = [&](int q) { return (int64_t)(p->q_start[q + 1] - p->q_start[q]) * p->G >= kPrefillRows; };
         const auto together = [&](int q, int q1) {  // end of the run of sequences from q on that are taken together
             while (q < q1 && !alone(q)) q++;
             return q;
@@ -455,9 +455,9 @@ tc_status tc_plan_set_shared(tc_plan *p, int32_t num_groups, const int32_t *seq_
             for (int q = seq_start[g], end; q < q1 && pages > 0; q = std::max(end, q + 1)) {
                 end = together(q, q1);
                 if (end - q < 2) continue;
-                const int row0 = p->q_start[q], rows = p->q_start[end] - row0, after = 1 << 30;
+                const int row0 = p->q_start[q], rows = p->q_start[end] - row0, after = INT32_MAX - 1023;  // (a block of rows ends before kNoToken)
                 const SpanRuns all = {pages, 0, 0, 0, 0, 0};
-                if (rows * p->G <= 16) {
+                if (rows <= 16 / p->G) {
                     s.entries.push_back({row0, rows * p->G, after, p->page_off[q], all, true});
                     continue;
                 }

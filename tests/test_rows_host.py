@@ -51,7 +51,9 @@ def test_refusals(tc, want, change):  # noqa: F811
     want = getattr(tc, want)
     if (want, change) not in [(getattr(tc, w), c) for w, c in REFUSALS_V]:
         assert abi._status(tc, lambda: tc.tc_qk_norm_rotate(plan, rows_of(tc, **change), 1 << 22, 1 << 23)) == want
+        assert "host-only" not in tc.last_error()
     assert abi._status(tc, lambda: tc.tc_qk_norm_rotate_append(plan, pool, rows_of(tc, **change), 1 << 22)) == want
+    assert "host-only" not in tc.last_error()
 
 
 def test_refusals_of_outputs_pools_and_plans(tc):  # noqa: F811
@@ -93,3 +95,26 @@ def test_rows_whose_heads_are_not_adjacent_are_refused(tc):  # noqa: F811
     x = torch.zeros(4, 8, 2, 64)
     with pytest.raises(ValueError):
         tc.make_qkv_rows(x[:, :, 0], x[:, :, 1])
+
+
+def test_strides_of_tensors(tc):  # noqa: F811
+    """A single token's stride says nothing; rows of two dimensions; freq and positions of another width."""
+    import torch
+    x = torch.zeros(1, 8, 64, dtype=torch.bfloat16)
+    rows = tc.make_qkv_rows(x.expand(1, 8, 64).as_strided((1, 8, 64), (7, 64, 1)), torch.zeros(3, 1024, dtype=torch.bfloat16)[:, 512:])
+    assert rows.q_stride == 512 and rows.k_stride == 1024
+    with pytest.raises(ValueError):
+        tc.make_qkv_rows(x, torch.zeros(1024, 3, dtype=torch.bfloat16).t())
+    with pytest.raises(ValueError):
+        tc.make_qkv_rows(x, x, freq=torch.zeros(32))
+    with pytest.raises(ValueError):
+        tc.make_qkv_rows(x, x, positions=torch.zeros(1, dtype=torch.int64))
+
+
+def test_rows_that_are_not_packed_are_not_their_own_output(tc):  # noqa: F811
+    plan = abi._plan(tc)
+    pool = tc.make_pool(8, 2, 128, 32, 1 << 20, 1 << 21)
+    wide = rows_of(tc, q=1 << 22, q_stride=8 * 128 + 8)
+    assert abi._status(tc, lambda: tc.tc_qk_norm_rotate(plan, wide, 1 << 22, 1 << 23)) == tc.TC_ERR_ARG and "packed" in tc.last_error()
+    assert abi._status(tc, lambda: tc.tc_qk_norm_rotate_append(plan, pool, wide, 1 << 22)) == tc.TC_ERR_ARG and "packed" in tc.last_error()
+    assert abi._status(tc, lambda: tc.tc_qk_norm_rotate(plan, rows_of(tc, k=1 << 23, k_stride=2 * 128 + 8), 1 << 22, 1 << 23)) == tc.TC_ERR_ARG and "packed" in tc.last_error()

@@ -7,7 +7,7 @@ import pytest
 import test_abi_host as abi
 from test_abi_host import tc  # noqa: F401  (the fixture)
 
-AFTER = 1 << 30
+AFTER = (1 << 31) - 1024
 
 
 def batch(q_len, ctx, groups=None, seed=0, spare=3):
@@ -269,3 +269,14 @@ def test_an_empty_batch_is_a_no_op(tc):  # noqa: F811
     for call in (tc.tc_window_attention, tc.tc_shared_attention):
         call(plan, pool, None, None, 0.0)
     assert plan.window_workspace_bytes == plan.shared_workspace_bytes == 0 and C.sizeof(tc.tc_span_info) == 64
+
+
+def test_a_window_past_32_bits_is_all_tokens(tc):  # noqa: F811
+    plan = abi._plan(tc)
+    lists = []
+    for window, sinks in (((1 << 31) - 1, (1 << 31) - 1), (1 << 32, 1 << 40)):
+        plan.set_window(window, sinks)
+        lists.append([plan.span_items(kind) for kind in (0, 1, 2)])
+    for a, b in zip(*lists):
+        assert np.array_equal(a, b)
+    assert abi._status(tc, lambda: plan.set_window((1 << 32) * -1 + 5)) == tc.TC_ERR_ARG
