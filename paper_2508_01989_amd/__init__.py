@@ -168,12 +168,14 @@ def _row_stride(x):
     """Elements from a token's heads to the next token's in a tensor [T][heads][D]; 0 for None or an address."""
     if x is None or isinstance(x, int):
         return 0
-    strides, token = x.stride(), 1
-    for n, stride in zip(reversed(x.shape[1:]), reversed(strides[1:])):
+    strides, shape, token = x.stride(), x.shape, 1
+    if len(shape) == 3 and strides[2] == 1 and strides[1] == shape[2] and shape[0] > 1:
+        return strides[0]
+    for n, stride in zip(reversed(shape[1:]), reversed(strides[1:])):
         if n > 1 and stride != token:
             raise ValueError("a token's heads must be adjacent")
         token *= n
-    return strides[0] if x.shape[0] > 1 else token
+    return strides[0] if shape[0] > 1 else token
 
 
 def make_qkv_rows(q, k, v=None, q_weight=None, k_weight=None, eps=1e-6, freq=None, rotary_dim=None, adjacent=False, positions=None,
@@ -181,9 +183,10 @@ def make_qkv_rows(q, k, v=None, q_weight=None, k_weight=None, eps=1e-6, freq=Non
     """Rows for tc_qk_norm_rotate: tensors [T][heads][D] whose heads are adjacent; a stride that is not given is the tensor's own.  rotary_dim: twice the length of freq unless given."""
     if rotary_dim is None:
         rotary_dim = 0 if freq is None else 2 * freq.numel()
-    for x, size, what in ((freq, 8, "freq is in 64-bit floating point"), (positions, 4, "positions are in 32 bits")):
-        if hasattr(x, "element_size") and x.element_size() != size:
-            raise ValueError(what)
+    if freq is not None and not isinstance(freq, int) and freq.element_size() != 8:
+        raise ValueError("freq is in 64-bit floating point")
+    if positions is not None and not isinstance(positions, int) and positions.element_size() != 4:
+        raise ValueError("positions are in 32 bits")
     return tc_qkv_rows(_ptr(q), _ptr(k), _ptr(v), _row_stride(q) if q_stride is None else q_stride, _row_stride(k) if k_stride is None else k_stride,
                        _row_stride(v) if v_stride is None else v_stride, _ptr(q_weight), _ptr(k_weight), eps, rotary_dim, _ptr(freq), adjacent, _ptr(positions))
 
