@@ -1,11 +1,16 @@
 // Attention over spans, beside the mixed attention of tc_attention.h and over the same pools in 16 bits: of each row over a window of its sequence's newest tokens and its
 // first ones (tc_window_attention), and of sequences that begin with the same cached tokens (tc_shared_attention), whose K and V are then read once for all of them.
 //
-//   span_attention_kernel  one launch for the whole batch: workgroups [0, n_sweeps) sweep K/V tiles for 256 (row, head) pairs of one KV head (prefill_item), the others run decode
-//                          items, up to 16 (row, head) pairs of one KV head over a range of pages that a wave, or several of a workgroup, stream into registers
+//   span_attention_kernel  one launch for the whole batch: n_sweeps workgroups sweep K/V tiles for 256 (row, head) pairs of one KV head, or 128 in workgroups of four waves (prefill_item),
+//                          the others run decode items, up to 16 (row, head) pairs of one KV head over a range of pages that a wave, or several of a workgroup, stream into registers
 //   span_merge_kernel      where the tokens of a row are shared out: its output from the partial results, out = sum_i 2^(m_i - m*) o_i / sum_i 2^(m_i - m*) l_i
 //
 // What a row attends over is a list of pages (SpanRuns) that begins with those that need no mask, so the main loops of both branches are those of attention over everything.
+//
+// Sweeps are bound by the matrix cores under the power limit, decodes by the stream from memory.  One MI355X, head_dim 128, bf16 unless stated: 8192 tokens over a window of 2048 and
+// 4 sinks, 64/8 heads, 500 us and 1.1 PFLOP/s (1.3 tile by tile: 1.6 us for 256 rows of every unit; 10 us of a block are not tiles); 128 decodes over 2048 and 16, 40/8, half, 155 us and
+// 6.5 TB/s; 2048 tokens and 64 decodes over 1000, 32/8, 68 us; 8 decodes over 1024 and 4, 8.5; 256 decodes behind 8192 shared tokens, 32/8, 124 us, 7 of it the combination (0.6 GB, where
+// every sequence for itself would read 9); 4 decodes behind 2048, 10.
 #include "tc_attention.h"
 
 namespace tc {
@@ -89,6 +94,7 @@ __device__ __forceinline__ void span_decode_sweep(const AttnArgs &A, int kvh, in
 
 // Vectors of four elements v0, v0 + step, .. of the output rows of a merge item, for KV head h: each from its row's partial results, i of them in workspace row
 // base + h * kv + i * step + r for row r of the item, for either of two lists.  PEER: other compute units have stored them while this kernel runs.
+// (As many requested at a time: 4 / 8 / 16, 33 decodes behind 1008 beside two groups more 17.2 / 16.3 / 16.6 us, 256 behind 8192 124 / 124 / 130, 4 behind 2048 10.1 / 10.2 / 10.8.)
 constexpr int kSpanMergeThreads = 256, kSpanMergeBatch = 8;
 template <int D, class E, bool PEER>
 __device__ __forceinline__ void span_merge_rows(const int32_t *it, int h, const float *ws, uint16_t *out, int64_t n_rows, int Hq, int G, int v0, int v_step) {
@@ -104,7 +110,8 @@ __device__ __forceinline__ void span_merge_rows(const int32_t *it, int h, const 
                 float2 ml[kSpanMergeBatch];
 #pragma unroll
                 for (int u = 0; u < kSpanMergeBatch; u++) {
-                    const int64_t at = base + min(i0 + u, n - 1) * step + r;
+                    if (i0 + u >= n) break;  // (uniform)
+                    const int64_t at = base + (i0 + u) * step + r;
                     o[u] = PEER ? load4<true>(win, ws, (uint32_t)((at * D + d) * sizeof(float))) : *reinterpret_cast<const f32x4 *>(ws + at * D + d);
                     ml[u] = load2<PEER>(ws_ml + at * 2);
                 }
