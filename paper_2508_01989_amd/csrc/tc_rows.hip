@@ -74,9 +74,10 @@ struct RowLane {
     }
 };
 
-// Head `h` of a row, four and four elements: norm, rotation by the angles whose cosines and sines are c and s.
+// Head `h` of a row, four and four elements: norm, and where the lane has rotated ones (`turns`) rotation by the angles whose cosines and sines are c and s.  (The others are not turned by
+// an angle of zero: x - y * 0 would take a NaN or an infinity from one to another, and a zero's sign.)
 template <int D, class E>
-__device__ __forceinline__ void turn_head(const RowsArgs &A, float (&a)[4], float (&b)[4], bool normed, const float (&w)[8], const float (&c)[4], const float (&s)[4]) {
+__device__ __forceinline__ void turn_head(const RowsArgs &A, bool turns, float (&a)[4], float (&b)[4], bool normed, const float (&w)[8], const float (&c)[4], const float (&s)[4]) {
     constexpr int LANES = D / 8;
     if (normed) {
         float sum = 0.f;
@@ -106,9 +107,9 @@ __device__ __forceinline__ void turn_head(const RowsArgs &A, float (&a)[4], floa
         }
     }
     const auto turn = [&](float &x, float &y, int pair) {
-        const float x0 = x;
-        x = x0 * c[pair] - y * s[pair];
-        y = y * c[pair] + x0 * s[pair];
+        const float x0 = x, y0 = y;
+        x = turns ? x0 * c[pair] - y0 * s[pair] : x0;
+        y = turns ? y0 * c[pair] + x0 * s[pair] : y0;
     };
     if (A.adjacent) {
         turn(a[0], a[1], 0);
@@ -280,7 +281,7 @@ __global__ void __launch_bounds__(kRowsThreads) rows_kernel(const RowsArgs A, co
                     angles(t, c, s);
                     widen4<E>(lo_now[u], a);
                     widen4<E>(hi_now[u], b);
-                    turn_head<D, E>(A, a, b, A.k_weight != nullptr, wk, c, s);
+                    turn_head<D, E>(A, lane.turns, a, b, A.k_weight != nullptr, wk, c, s);
                     char *const to = tile + sl.head * (LANES * 272) + (tok0 + t) * 16;
                     *reinterpret_cast<u32x2 *>(to + (lane.a >> 3) * 272 + (lane.a & 7) * 2) = narrow4<E>(a);
                     *reinterpret_cast<u32x2 *>(to + (lane.b >> 3) * 272 + (lane.b & 7) * 2) = narrow4<E>(b);
@@ -313,7 +314,7 @@ __global__ void __launch_bounds__(kRowsThreads) rows_kernel(const RowsArgs A, co
                 float a[4], b[4];
                 widen4<E>(lo_now[u], a);
                 widen4<E>(hi_now[u], b);
-                turn_head<D, E>(A, a, b, normed, w, c, s);
+                turn_head<D, E>(A, lane.turns, a, b, normed, w, c, s);
                 *reinterpret_cast<u32x2 *>(dst + h * head_stride + at_a) = narrow4<E>(a);
                 *reinterpret_cast<u32x2 *>(dst + h * head_stride + at_b) = narrow4<E>(b);
             }

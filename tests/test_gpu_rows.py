@@ -222,3 +222,26 @@ def test_in_a_graph_and_on_another_stream(tc):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(d.q_out2[:-1], q[:-1]) and torch.equal(d.k_pool, kp) and torch.equal(d.v_pool, vp)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("D, rotary", [(128, 0), (128, 48), (64, 0), (64, 24)])
+def test_elements_behind_the_rotated_ones_keep_every_bit(tc, D, rotary, adjacent, dtype):
+    """Without a weight the rest of a head is a copy: infinities, NaN, zeros of either sign and the smallest numbers reach no other element."""
+    nan, inf = (0x7E00, 0x7C00) if dtype == "fp16" else (0x7FC0, 0x7F80)
+    c = Case(6, 3, D, [1, 20, 1], [100, 7, 3], dtype, rotary, adjacent)
+    rng = np.random.default_rng(D + rotary)
+    some = rng.random(c.rows.shape) < 0.2
+    some[..., :rotary] = False
+    c.rows[some] = rng.choice(np.array([nan, inf, inf | 0x8000, 0x8000, 0, 1, 0x8001], np.uint16), int(some.sum()))
+    d = Device(tc, c)
+    rows = d.of((False, False))
+    tc.tc_qk_norm_rotate(d.plan, rows, d.q_out, d.k_out)
+    for which, t in ((0, d.q_out), (1, d.k_out)):
+        assert np.array_equal(d.host(t)[:-1][..., rotary:], c.parts()[which][..., rotary:])
+        want, size = norm_rotate(kvq.widen(np.ascontiguousarray(c.parts()[which][..., :rotary]), dtype), None, EPS, c.freq, rotary, adjacent, c.positions)
+        assert np.all(np.abs(d.values(t)[..., :rotary] - want) <= HALF_STEP[dtype] * np.abs(want) + 32 * 2.0 ** -24 * (1 + HALF_STEP[dtype]) * size + SMALLEST[dtype])
+    tc.tc_qk_norm_rotate_append(d.plan, d.pool, rows, d.q_out2)
+    tc.tc_kv_append(d.plan, d.ref, d.k_out, d.rows[:, c.Hq + c.Hkv:].contiguous())
+    assert np.array_equal(d.host(d.q_out), d.host(d.q_out2)) and np.array_equal(d.host(d.k_pool), d.host(d.k_ref)) and np.array_equal(d.host(d.v_pool), d.host(d.v_ref))
