@@ -100,10 +100,11 @@ __device__ __forceinline__ void turn_head(const RowsArgs &A, bool turns, float (
             }
             r = 1.f;
         }
+        // (The quotient first: it is sqrt(D) at most, while the root times a weight may leave 32 bits where the result does not.)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            a[e] *= r * w[e];
-            b[e] *= r * w[4 + e];
+            a[e] = a[e] * r * w[e];
+            b[e] = b[e] * r * w[4 + e];
         }
     }
     const auto turn = [&](float &x, float &y, int pair) {

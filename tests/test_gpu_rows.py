@@ -245,3 +245,25 @@ def test_elements_behind_the_rotated_ones_keep_every_bit(tc, D, rotary, adjacent
     tc.tc_qk_norm_rotate_append(d.plan, d.pool, rows, d.q_out2)
     tc.tc_kv_append(d.plan, d.ref, d.k_out, d.rows[:, c.Hq + c.Hkv:].contiguous())
     assert np.array_equal(d.host(d.q_out), d.host(d.q_out2)) and np.array_equal(d.host(d.k_pool), d.host(d.k_ref)) and np.array_equal(d.host(d.v_pool), d.host(d.v_ref))
+
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_weights_at_the_ends_of_the_type(tc, adjacent):
+    """Rows of 2^-46 and 2^46 with weights of 2^100 and 2^-100, and elements that are zero: the root and the weight lie apart by more than 32 bits hold, the results do not."""
+    c = Case(4, 2, 128, [1, 20], [9, 100], "bf16", None, adjacent)
+    rng = np.random.default_rng(4)
+    x = rng.standard_normal(c.rows.shape) * np.exp2(rng.choice([-46, 0, 46], c.rows.shape[:1]))[:, None, None]
+    x[rng.random(x.shape) < 0.1] = 0
+    c.rows = bits_of(x.astype(np.float32), "bf16")
+    c.weights = [bits_of(((1 + 0.3 * rng.standard_normal(128)) * np.exp2(rng.choice([-100, 0, 100], 128))).astype(np.float32), "bf16") for _ in range(2)]
+    d = Device(tc, c)
+    eps = float(np.float32(1e-37))
+    a = c.Hq
+    rows = tc.make_qkv_rows(d.rows[:, :a], d.rows[:, a:a + 2], d.rows[:, a + 2:], d.weights[0], d.weights[1], eps, d.freq, adjacent=adjacent)
+    tc.tc_qk_norm_rotate(d.plan, rows, d.q_out, d.k_out)
+    for which, t in ((0, d.q_out), (1, d.k_out)):
+        want, size = norm_rotate(kvq.widen(np.ascontiguousarray(c.parts()[which]), "bf16"), kvq.widen(c.weights[which], "bf16"), eps, c.freq, 128, adjacent, c.positions)
+        bound = HALF_STEP["bf16"] * np.abs(want) + 32 * 2.0 ** -24 * (1 + HALF_STEP["bf16"]) * size + SMALLEST["bf16"]
+        got = d.values(t)
+        assert np.all(np.abs(got - want) <= bound), (int(np.isnan(got).sum()), float(np.nanmax(np.abs(got - want) / bound)))
