@@ -183,10 +183,16 @@ def make_qkv_rows(q, k, v=None, q_weight=None, k_weight=None, eps=1e-6, freq=Non
     """Rows for tc_qk_norm_rotate: tensors [T][heads][D] whose heads are adjacent; a stride that is not given is the tensor's own.  rotary_dim: twice the length of freq unless given."""
     if rotary_dim is None:
         rotary_dim = 0 if freq is None else 2 * freq.numel()
-    if freq is not None and not isinstance(freq, int) and freq.element_size() != 8:
-        raise ValueError("freq is in 64-bit floating point")
-    if positions is not None and not isinstance(positions, int) and positions.element_size() != 4:
-        raise ValueError("positions are in 32 bits")
+    if freq is not None and not isinstance(freq, int):
+        if freq.element_size() != 8 or not freq.is_floating_point():
+            raise ValueError("freq is in 64-bit floating point")
+        if 2 * freq.numel() < rotary_dim or not freq.is_contiguous():
+            raise ValueError("freq has rotary_dim / 2 adjacent elements")
+    if positions is not None and not isinstance(positions, int):
+        if positions.element_size() != 4 or positions.is_floating_point():
+            raise ValueError("positions are integers in 32 bits")
+        if not positions.is_contiguous():
+            raise ValueError("positions are adjacent")
     return tc_qkv_rows(_ptr(q), _ptr(k), _ptr(v), _row_stride(q) if q_stride is None else q_stride, _row_stride(k) if k_stride is None else k_stride,
                        _row_stride(v) if v_stride is None else v_stride, _ptr(q_weight), _ptr(k_weight), eps, rotary_dim, _ptr(freq), adjacent, _ptr(positions))
 

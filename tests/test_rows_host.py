@@ -118,3 +118,17 @@ def test_rows_that_are_not_packed_are_not_their_own_output(tc):  # noqa: F811
     assert abi._status(tc, lambda: tc.tc_qk_norm_rotate(plan, wide, 1 << 22, 1 << 23)) == tc.TC_ERR_ARG and "packed" in tc.last_error()
     assert abi._status(tc, lambda: tc.tc_qk_norm_rotate_append(plan, pool, wide, 1 << 22)) == tc.TC_ERR_ARG and "packed" in tc.last_error()
     assert abi._status(tc, lambda: tc.tc_qk_norm_rotate(plan, rows_of(tc, k=1 << 23, k_stride=2 * 128 + 8), 1 << 22, 1 << 23)) == tc.TC_ERR_ARG and "packed" in tc.last_error()
+
+
+def test_frequencies_and_positions_that_do_not_fit_are_refused(tc):  # noqa: F811
+    """The kernel reads rotary_dim / 2 adjacent frequencies, and adjacent positions: fewer of them, others in between or another type would be read behind the end or wrongly."""
+    import torch
+    x = torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    freq, positions = torch.ones(32, dtype=torch.float64), torch.zeros(3, dtype=torch.int32)
+    for kw in (dict(freq=freq, rotary_dim=72), dict(freq=freq[:3], rotary_dim=8), dict(freq=freq[::2]), dict(freq=freq[:1].expand(8)), dict(freq=torch.ones(32, dtype=torch.int64)),
+               dict(positions=positions.float()), dict(positions=torch.zeros(6, dtype=torch.int32)[::2]), dict(positions=positions[:1].expand(3))):
+        with pytest.raises(ValueError):
+            tc.make_qkv_rows(x, x, **kw)
+    rows = tc.make_qkv_rows(x, x, freq=freq, rotary_dim=16, positions=positions)  # more of them are no harm
+    assert rows.rotary_dim == 16 and rows.freq == freq.data_ptr() and rows.positions == positions.data_ptr()
+    assert tc.make_qkv_rows(x, x, freq=freq).rotary_dim == 64 and tc.make_qkv_rows(x, x, freq=1 << 20, rotary_dim=128).rotary_dim == 128
