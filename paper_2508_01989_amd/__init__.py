@@ -140,10 +140,12 @@ def _check(status):
 
 def _ptr(x):
     """Device (or host) address of a torch tensor / numpy array / int / None."""
+    if x is None:
+        return None
     try:
         return x.data_ptr()
     except AttributeError:
-        return x if x is None or isinstance(x, int) else x.ctypes.data
+        return x if isinstance(x, int) else x.ctypes.data
 
 
 def _stream(stream):
@@ -169,8 +171,6 @@ def _row_stride(x):
     if x is None or isinstance(x, int):
         return 0
     strides, shape, token = x.stride(), x.shape, 1
-    if len(shape) == 3 and strides[2] == 1 and strides[1] == shape[2] and shape[0] > 1:
-        return strides[0]
     for n, stride in zip(reversed(shape[1:]), reversed(strides[1:])):
         if n > 1 and stride != token:
             raise ValueError("a token's heads must be adjacent")
@@ -178,14 +178,73 @@ def _row_stride(x):
     return strides[0] if shape[0] > 1 else token
 
 
+_row_types, _freq_types = set(), set()  # types of tensors that have been found right for rows and for frequencies
+
+
+def _check_types(*tensors):
+    """ValueError unless all of them are of one type in 16 bits (integers are patterns, of any)."""
+    kind = None
+    for x in tensors:
+        if x is None or isinstance(x, int) or x.dtype is kind:
+            continue
+        if x.element_size() != 2:
+            raise ValueError("q, k, v and the weights are in 16 bits")
+        if x.is_floating_point():
+            if kind is not None:
+                raise ValueError("q, k, v and the weights are of one type")
+            kind = x.dtype
+    if kind is not None:
+        _row_types.add(kind)
+
+
+def _usual_rows(q, k, v, q_weight, k_weight):
+    """The first eight fields of a call like most, in half of the time that every case takes: tensors of three dimensions, of one type that is known, with weights that fit.  None for other calls."""
+    try:
+        kind = q.dtype
+        if kind not in _row_types or k.dtype is not kind:
+            return None
+        tokens, _, width = q.shape
+        q_stride, head, element = q.stride()
+        if tokens < 2 or head != width or element != 1:
+            return None
+        tokens, _, w = k.shape
+        k_stride, head, element = k.stride()
+        if tokens < 2 or w != width or head != width or element != 1:
+            return None
+        v_ptr, v_stride = None, 0
+        if v is not None:
+            tokens, _, w = v.shape
+            v_stride, head, element = v.stride()
+            if v.dtype is not kind or tokens < 2 or w != width or head != width or element != 1:
+                return None
+            v_ptr = v.data_ptr()
+        for w in (q_weight, k_weight):
+            if w is not None and (w.dtype is not kind or w.numel() != width or not w.is_contiguous()):
+                return None
+        return (q.data_ptr(), k.data_ptr(), v_ptr, q_stride, k_stride, v_stride, None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr())
+    except (AttributeError, ValueError):  # an address, other dimensions
+        return None
+
+
 def make_qkv_rows(q, k, v=None, q_weight=None, k_weight=None, eps=1e-6, freq=None, rotary_dim=None, adjacent=False, positions=None,
                   q_stride=None, k_stride=None, v_stride=None) -> tc_qkv_rows:
-    """Rows for tc_qk_norm_rotate: tensors [T][heads][D] whose heads are adjacent; a stride that is not given is the tensor's own.  rotary_dim: twice the length of freq unless given."""
+    """Rows for tc_qk_norm_rotate: tensors [T][heads][D] whose heads are adjacent; a stride that is not given is the tensor's own.  rotary_dim: twice the length of freq unless given.
+    Weights are of the rows' type.  ValueError for tensors of other types or sizes (addresses are taken as they are)."""
+    first = _usual_rows(q, k, v, q_weight, k_weight) if q_stride is k_stride is v_stride is None else None
+    if first is None:
+        _check_types(q, k, v, q_weight, k_weight)
+        for x, w in ((q, q_weight), (k, k_weight)):
+            if w is not None and not isinstance(w, int) and (not w.is_contiguous() or (x is not None and not isinstance(x, int) and x.dim() == 3 and w.numel() != x.shape[2])):
+                raise ValueError("a weight has head_dim adjacent elements")
+        first = (_ptr(q), _ptr(k), _ptr(v), _row_stride(q) if q_stride is None else q_stride, _row_stride(k) if k_stride is None else k_stride,
+                 _row_stride(v) if v_stride is None else v_stride, _ptr(q_weight), _ptr(k_weight))
     if rotary_dim is None:
         rotary_dim = 0 if freq is None else 2 * freq.numel()
     if freq is not None and not isinstance(freq, int):
-        if freq.element_size() != 8 or not freq.is_floating_point():
-            raise ValueError("freq is in 64-bit floating point")
+        if freq.dtype not in _freq_types:
+            if freq.element_size() != 8 or not freq.is_floating_point():
+                raise ValueError("freq is in 64-bit floating point")
+            _freq_types.add(freq.dtype)
         if 2 * freq.numel() < rotary_dim or not freq.is_contiguous():
             raise ValueError("freq has rotary_dim / 2 adjacent elements")
     if positions is not None and not isinstance(positions, int):
@@ -193,8 +252,7 @@ def make_qkv_rows(q, k, v=None, q_weight=None, k_weight=None, eps=1e-6, freq=Non
             raise ValueError("positions are integers in 32 bits")
         if not positions.is_contiguous():
             raise ValueError("positions are adjacent")
-    return tc_qkv_rows(_ptr(q), _ptr(k), _ptr(v), _row_stride(q) if q_stride is None else q_stride, _row_stride(k) if k_stride is None else k_stride,
-                       _row_stride(v) if v_stride is None else v_stride, _ptr(q_weight), _ptr(k_weight), eps, rotary_dim, _ptr(freq), adjacent, _ptr(positions))
+    return tc_qkv_rows(*first, eps, rotary_dim, _ptr(freq), adjacent, _ptr(positions))
 
 
 def _shape(pool):

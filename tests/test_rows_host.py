@@ -132,3 +132,22 @@ def test_frequencies_and_positions_that_do_not_fit_are_refused(tc):  # noqa: F81
     rows = tc.make_qkv_rows(x, x, freq=freq, rotary_dim=16, positions=positions)  # more of them are no harm
     assert rows.rotary_dim == 16 and rows.freq == freq.data_ptr() and rows.positions == positions.data_ptr()
     assert tc.make_qkv_rows(x, x, freq=freq).rotary_dim == 64 and tc.make_qkv_rows(x, x, freq=1 << 20, rotary_dim=128).rotary_dim == 128
+
+
+def test_rows_and_weights_of_another_type_are_refused(tc):  # noqa: F811
+    """Weights in 32 bits, as checkpoints often hold them, would be read as patterns of 16; so would weights in the other 16-bit type, and rows of either kind."""
+    import torch
+    x, w = torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.ones(64, dtype=torch.bfloat16)
+    make = tc.make_qkv_rows
+    for q, k, v, kw in ((x, x, None, dict(q_weight=w.float())), (x, x, None, dict(k_weight=w.double())), (x, x, None, dict(k_weight=w.half())), (x, x.half(), None, {}), (x, x, x.half(), {}),
+                        (x.float(), x.float(), None, {}), (x, x.float(), None, {}), (x, x, x.float(), {}), (1 << 20, x.float(), None, dict(q_stride=128)),
+                        (1 << 20, x, None, dict(q_stride=128, k_weight=w.half())), (x.view(torch.int16), x.view(torch.int16), None, dict(q_weight=w, k_weight=w.half())), (1 << 20, 1 << 21, None, dict(q_stride=128, k_stride=128, q_weight=w.float()))):
+        with pytest.raises(ValueError):
+            make(q, k, v, **kw)
+    for kw in (dict(q_weight=w[:32]), dict(k_weight=torch.ones(128, dtype=torch.bfloat16)), dict(q_weight=torch.ones(128, dtype=torch.bfloat16)[::2]), dict(k_weight=w[:1].expand(64))):
+        with pytest.raises(ValueError):  # a weight for each element of a head, one after the other
+            make(x, x, **kw)
+    bits = x.view(torch.int16)  # patterns, whose type nothing says
+    for q, k, v, a, b in ((x, x, x, w, w), (bits, bits, bits, w, w), (x, bits, None, w.view(torch.int16), None), (x.view(3, 128), x, x, w, w)):
+        rows = make(q, k, v, a, b)
+        assert (rows.q, rows.q_weight, rows.k_weight) == (q.data_ptr(), a.data_ptr(), None if b is None else b.data_ptr())
