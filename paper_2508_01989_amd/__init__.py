@@ -229,7 +229,8 @@ def _usual_rows(q, k, v, q_weight, k_weight):
 def make_qkv_rows(q, k, v=None, q_weight=None, k_weight=None, eps=1e-6, freq=None, rotary_dim=None, adjacent=False, positions=None,
                   q_stride=None, k_stride=None, v_stride=None) -> tc_qkv_rows:
     """Rows for tc_qk_norm_rotate: tensors [T][heads][D] whose heads are adjacent; a stride that is not given is the tensor's own.  rotary_dim: twice the length of freq unless given.
-    Weights are of the rows' type.  ValueError for tensors of other types or sizes (addresses are taken as they are)."""
+    Weights are of the rows' type.  ValueError for tensors of other types or sizes (addresses are taken as they are).
+    The rows hold the tensors that they are made of."""
     first = _usual_rows(q, k, v, q_weight, k_weight) if q_stride is k_stride is v_stride is None else None
     if first is None:
         _check_types(q, k, v, q_weight, k_weight)
@@ -252,7 +253,9 @@ def make_qkv_rows(q, k, v=None, q_weight=None, k_weight=None, eps=1e-6, freq=Non
             raise ValueError("positions are integers in 32 bits")
         if not positions.is_contiguous():
             raise ValueError("positions are adjacent")
-    return tc_qkv_rows(*first, eps, rotary_dim, _ptr(freq), adjacent, _ptr(positions))
+    rows = tc_qkv_rows(*first, eps, rotary_dim, _ptr(freq), adjacent, _ptr(positions))
+    rows.tensors = q, k, v, q_weight, k_weight, freq, positions  # (the addresses are used by calls to come)
+    return rows
 
 
 def _shape(pool):

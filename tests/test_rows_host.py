@@ -151,3 +151,24 @@ def test_rows_and_weights_of_another_type_are_refused(tc):  # noqa: F811
     for q, k, v, a, b in ((x, x, x, w, w), (bits, bits, bits, w, w), (x, bits, None, w.view(torch.int16), None), (x.view(3, 128), x, x, w, w)):
         rows = make(q, k, v, a, b)
         assert (rows.q, rows.q_weight, rows.k_weight) == (q.data_ptr(), a.data_ptr(), None if b is None else b.data_ptr())
+
+
+def test_rows_hold_their_tensors(tc):  # noqa: F811
+    """What a call is given may be made in the call: it lives as long as the rows do."""
+    import gc
+    import weakref
+
+    import torch
+    for wide in (False, True):  # the usual call and any other
+        x = [torch.zeros(3, 2, 64, dtype=torch.bfloat16) for _ in range(3)]
+        x = [t.view(3, 128) for t in x] if wide else x
+        more = [torch.ones(64, dtype=torch.bfloat16), torch.ones(64, dtype=torch.bfloat16), torch.ones(32, dtype=torch.float64), torch.zeros(3, dtype=torch.int32)]
+        refs = [weakref.ref(t) for t in x + more]
+        rows = tc.make_qkv_rows(*x, more[0], more[1], freq=more[2], positions=more[3])
+        del x, more
+        gc.collect()
+        assert all(r() is not None for r in refs)
+        assert rows.positions == refs[-1]().data_ptr()
+        del rows
+        gc.collect()
+        assert all(r() is None for r in refs)
