@@ -330,7 +330,7 @@ tc_status tc_window_attention(const tc_plan *plan, const tc_kv_pool *pool, const
  * Attention of sequences that begin with the same cached tokens: the same result as tc_mixed_attention's, up to rounding, but the K and V of what a group of sequences shares are
  * read once for all of its rows, as one matrix product, and not once for each.  Group g is the sequences seq_start[g] .. seq_start[g + 1] - 1 of the batch
  * (HOST [num_groups + 1], from 0 to num_seqs, strictly increasing), which share their first prefix_len[g] tokens (HOST [num_groups], a multiple of 16, 0 for a
- * group that shares nothing): no more than any of them has cached (TC_ERR_SPAN), in the same blocks (TC_ERR_BLOCK).  Everything else is as for the window above.
+ * group that shares nothing): no more than any of them has cached and than 2^31 - 1024 (TC_ERR_SPAN), in the same blocks (TC_ERR_BLOCK).  Everything else is as for the window above.
  */
 tc_status tc_plan_set_shared(tc_plan *plan, int32_t num_groups, const int32_t *seq_start, const int32_t *prefix_len, void *stream);
 size_t tc_shared_workspace_bytes(const tc_plan *plan);

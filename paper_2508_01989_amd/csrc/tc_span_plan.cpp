@@ -17,6 +17,7 @@ tc_status fail(tc_status s, const char *msg) {
 }
 
 constexpr int kTilePages = kPrefillTileTokens / kBlock;
+constexpr int32_t kBehindAll = INT32_MAX - 1023;  // position of the rows that sweep shared tokens: behind these, and the last of a block of rows before kNoToken
 constexpr int kMinSweepTiles = 4;   // a piece of a cut sweep is not shorter than this
 constexpr double kAloneSmall = 0.6;  // a tile of a workgroup of four waves that has its compute unit to itself, to one of eight's
 constexpr double kPieceUs = 8, kMergeUs = 8, kPartUs = 0.15;  // what a piece costs on top of its tiles: its start and end; the launch that combines pieces, and what each piece of a row adds to it
@@ -455,14 +456,15 @@ tc_status tc_plan_set_shared(tc_plan *p, int32_t num_groups, const int32_t *seq_
             for (int q = seq_start[g], end; q < q1 && pages > 0; q = std::max(end, q + 1)) {
                 end = together(q, q1);
                 if (end - q < 2) continue;
-                const int row0 = p->q_start[q], rows = p->q_start[end] - row0, after = INT32_MAX - 1023;  // (a block of rows ends before kNoToken)
+                if (prefix_len[g] > kBehindAll) return fail(TC_ERR_SPAN, "more than 2^31 - 1024 shared tokens");
+                const int row0 = p->q_start[q], rows = p->q_start[end] - row0;
                 const SpanRuns all = {pages, 0, 0, 0, 0, 0};
                 if (rows <= 16 / p->G) {
-                    s.entries.push_back({row0, rows * p->G, after, p->page_off[q], all, true});
+                    s.entries.push_back({row0, rows * p->G, kBehindAll, p->page_off[q], all, true});
                     continue;
                 }
                 const int per = s.rows_per_block() / p->G;
-                for (int i = 0; i < rows; i += per) s.blocks.push_back({row0 + i, std::min(per, rows - i), after, p->page_off[q], all, true});
+                for (int i = 0; i < rows; i += per) s.blocks.push_back({row0 + i, std::min(per, rows - i), kBehindAll, p->page_off[q], all, true});
             }
         }
         const size_t n_blocks = s.blocks.size(), n_entries = s.entries.size();

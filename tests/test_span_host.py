@@ -280,3 +280,14 @@ def test_a_window_past_32_bits_is_all_tokens(tc):  # noqa: F811
     for a, b in zip(*lists):
         assert np.array_equal(a, b)
     assert abi._status(tc, lambda: plan.set_window((1 << 32) * -1 + 5)) == tc.TC_ERR_ARG
+
+
+def test_shared_tokens_past_the_position_behind_all_tokens_are_refused(tc):  # noqa: F811
+    """A sweep takes its rows to be behind what they share, at 2^31 - 1024: the tokens from there on would be left out."""
+    shared = (1 << 31) - 80
+    table = np.zeros((2, shared // 16 + 1), np.int32)
+    plan = tc.Plan(tc.make_pool(8, 1, 64, 1), np.array([0, 2, 3], np.int32), np.array([shared, shared], np.int32), table, host_only=True)
+    assert abi._status(tc, lambda: plan.set_shared([0, 2], [shared])) == tc.TC_ERR_SPAN
+    assert abi._status(tc, lambda: plan.set_shared([0, 2], [AFTER + 16])) == tc.TC_ERR_SPAN
+    plan.set_shared([0, 2], [AFTER])
+    assert plan.span_items(0, True)[:, 11].min() == AFTER  # (and the own position of the chunk)
