@@ -267,3 +267,9 @@ def test_weights_at_the_ends_of_the_type(tc, adjacent):
         bound = HALF_STEP["bf16"] * np.abs(want) + 32 * 2.0 ** -24 * (1 + HALF_STEP["bf16"]) * size + SMALLEST["bf16"]
         got = d.values(t)
         assert np.all(np.abs(got - want) <= bound), (int(np.isnan(got).sum()), float(np.nanmax(np.abs(got - want) / bound)))
+
+
+@pytest.mark.parametrize("D, heads, dtype", [(128, (5, 1), "bf16"), (64, (4, 2), "fp16")])
+def test_a_workgroup_to_each_page(tc, D, heads, dtype):
+    """A chunk of so many pages that each has one workgroup, whose waves take one task after the other."""
+    check(tc, Case(*heads, D, [6400, 1], [13, 5], dtype))
