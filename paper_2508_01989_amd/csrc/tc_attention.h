@@ -1225,12 +1225,17 @@ __device__ __forceinline__ void prefill_item(const AttnArgs &A, const int32_t *_
         W::load_k((lds_cptr)(lds_k + k_lane_off), 0, kf);
         W::qk(kf, qreg, sc);
         W::load_k((lds_cptr)(lds_k + k_lane_off), 1, kf);
-        // the first phase has no earlier half to accumulate: give its P V product zero probabilities
-        W::load_v((lds_cptr)(lds_v + v_lane_off), 0, vf);
+        // the first phase has no earlier half to accumulate: give its P V product zero probabilities, of a span zero operands too (V may be infinite, and zero times that is NaN)
+        if constexpr (!SPAN) W::load_v((lds_cptr)(lds_v + v_lane_off), 0, vf);
 #pragma unroll
-        for (int b = 0; b < 2; b++)
+        for (int b = 0; b < 2; b++) {
 #pragma unroll
             for (int e = 0; e < 8; e++) pb[b][e] = (el)0.f;
+            if constexpr (SPAN) {
+#pragma unroll
+                for (int c = 0; c < MT; c++) vf[b][c] = pb[b];
+            }
+        }
         if (SPAN ? t_begin >= plain_tiles : t_begin * C::kTileTokens + 31 > wave_pmin) mask(sc, t_begin * C::kTileTokens);
         m_run = next_reference_max(m_run, W::row_max(sc) * c_log2);  // the first half-tile's true maxima
         const std::true_type yes;
