@@ -312,7 +312,8 @@ tc_status tc_qk_norm_rotate_append(const tc_plan *plan, const tc_kv_pool *pool, 
  * Attention over a window: row t at position p attends over the tokens j <= p of its sequence with p - j < window or j < sinks, its newest `window` tokens (itself
  * among them) and the first ones, as in models whose layers look back a fixed distance, and in streams that outgrow what is kept.
  * tc_plan_set_window makes the work list for the plan's batch and uploads it on `stream`; it holds until the next tc_plan_set_window or tc_plan_update of the plan
- * (after which it is made anew; in steady state that allocates nothing).  The rules of tc_plan_update about streams and earlier calls go for it too.  The
+ * (after which it is made anew; in steady state that allocates nothing).  The rules of tc_plan_update about streams and earlier calls go for it too: calls captured into a graph are
+ * of the list as it was, and are not replayed once it has been made anew.  The
  * plan serves tc_mixed_attention as before, so that layers of both kinds share it.  window >= 1, sinks >= 0 (TC_ERR_ARG); plans for pools in 16 bits (TC_ERR_SHAPE).
  *
  * tc_window_attention is then tc_mixed_attention with that mask: same arguments, accumulation and roundings (TC_ERR_ARG before tc_plan_set_window).  Of the cache, only blocks

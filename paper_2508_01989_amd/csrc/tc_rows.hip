@@ -3,8 +3,9 @@
 //
 //   y = x * (mean(x^2) + eps)^-1/2 * w,   then (a, b) -> (a cos t - b sin t, b cos t + a sin t)  for each pair, t = position * freq[pair]
 //
-// Bound by the bytes: every element is read once and written once, 2 bytes each way.  One MI355X, head_dim 128: 8192 tokens, 64/8 heads, 68 us and 4.9 TB/s with the append, 54 us and 5.6
-// without (a bare copy 5.1); 512 decodes, 40/8, 9.0 and 5.2 us; 8 decodes 4.3, the launch and a chain of three accesses to memory.
+// Bound by the bytes: every element is read once and written once, 2 bytes each way; v and k of a single token go into the pages in pieces of 2 and 16 bytes, for each of which memory
+// takes 32 (512 decodes, 40/8 heads, write 24 MB by the counters where they have 7.3).  One MI355X, head_dim 128, launches back to back in a graph: 8192 tokens, 64/8, 67-70 us and 4.8-5.0 TB/s
+// with the append, 56 us and 5.4 without (a bare copy 5.0); 512 decodes, 40/8, 8.9 and 5.2 us; 8 decodes 4.6 and 3.9, the launch and a chain of three accesses to memory.
 #include "tc_attention.h"
 
 namespace tc {
@@ -354,9 +355,9 @@ int launch_rows(const tc_plan *p, const tc_kv_pool *pool, const tc_qkv_rows *row
     A.rotary_dim = rows->rotary_dim;
     A.adjacent = rows->adjacent;
     A.eps = rows->eps;
-    // A workgroup a segment where there are enough of them, for the fewer angles (8192 tokens, 512 segments, 68 us; two workgroups each 75, four 71); else as many as have a task
-    // for each wave (1234 tokens, 32/32 heads, head_dim 64, 94 segments: one 15.5 us, four 7.5, eight 6.5).  Single tokens: two, whose waves store fewer elements of v each
-    // (512 of them, 40/8 heads, head_dim 128, one 9.1 us, two 8.7, three 9.5; 8 of them, 32/8, one 4.9, two 4.2).
+    // A workgroup a segment where there are enough of them, for the fewer angles (8192 tokens, 512 segments, 68 us; two workgroups each 75, four 73); else as many as have a task
+    // for each wave (1234 tokens, 32/32 heads, head_dim 64, 94 segments: one 15.8 us, four 7.7, eight 6.6).  Single tokens: two, whose waves store fewer elements of v each
+    // (512 of them, 40/8 heads, head_dim 128, one 9.3 us, two 9.0, three 9.8; 8 of them, 32/8, one 4.8, two 4.6).
     const int chunk = 64 / (p->D / 8) * kRowsBatch, most = (kBlock * ((p->Hq + chunk - 1) / chunk + (p->Hkv + chunk - 1) / chunk) + kRowsThreads / 64 - 1) / (kRowsThreads / 64);
     A.splits = p->n_append_prefill > 0 ? (int)std::min<int64_t>(most, std::max<int64_t>(1, kRowsWorkgroups / p->n_append)) : 2;
     const dim3 grid((unsigned)p->n_append, (unsigned)A.splits);

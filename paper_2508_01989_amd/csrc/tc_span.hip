@@ -7,10 +7,10 @@
 //
 // What a row attends over is a list of pages (SpanRuns) that begins with those that need no mask, so the main loops of both branches are those of attention over everything.
 //
-// Sweeps are bound by the matrix cores under the power limit, decodes by the stream from memory.  One MI355X, head_dim 128, bf16 unless stated: 8192 tokens over a window of 2048 and
-// 4 sinks, 64/8 heads, 500 us and 1.1 PFLOP/s (1.3 tile by tile: 1.6 us for 256 rows of every unit; 10 us of a block are not tiles); 128 decodes over 2048 and 16, 40/8, half, 155 us and
-// 6.5 TB/s; 2048 tokens and 64 decodes over 1000, 32/8, 68 us; 8 decodes over 1024 and 4, 8.5; 256 decodes behind 8192 shared tokens, 32/8, 124 us, 7 of it the combination (0.6 GB, where
-// every sequence for itself would read 9); 4 decodes behind 2048, 10.
+// Sweeps are bound by the matrix cores under the power limit, decodes by the stream from memory.  One MI355X, head_dim 128, bf16 unless stated, calls back to back: 8192 tokens over a window
+// of 2048 and 4 sinks, 64/8 heads, 496-533 us and 1.0-1.1 PFLOP/s (1.26 tile by tile: 1.71 us for 256 rows of every unit, from windows of 2048 to 8192; 10 us of a block are not tiles);
+// 128 decodes over 2048 and 16, 40/8, half, 152-156 us and 6.5-6.7 TB/s; 2048 tokens and 64 decodes over 1000, 32/8, 68-71 us; 8 decodes over 1024 and 4, 10; 256 decodes behind 8192 shared
+// tokens, 32/8, 124 us, 7 of it the combination (0.69 GB read by the counters, where every sequence for itself would read 9); 4 decodes behind 2048, 11.
 #include "tc_attention.h"
 
 namespace tc {
